@@ -337,6 +337,171 @@ int anakin_rollout_noalloc(const anakin_cfg* cfg, uint64_t seed, int64_t global_
  */
 int anakin_noalloc_status(void* cuda_stream, int* device_status);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Policies over token vocabularies.  (The paper has no counterpart: its agents choose among a handful of actions.  These calls carry the
+ * objectives of anakin_learn_ppo to policies whose action is one of V tokens and whose trajectories are sequences of any length.)
+ *
+ * Stateless: no handle.  The caller passes DEVICE pointers and the stream; every call enqueues kernels on `cuda_stream` and returns
+ * without synchronising, allocates nothing, and may be captured into a CUDA graph.  The device that is current at the call must be the
+ * one that the pointers and the stream belong to.  All calls are thread-safe.  Calls that take a workspace use it for that one call: two
+ * that may run at the same time (on two streams, or replays of two graphs) need one each.  Nothing is kept from one call to the next, and
+ * the same inputs give the same bits on the same kind of GPU.
+ *
+ * Rows.  A row of the logits is the distribution of one token; the rows of all sequences lie one after the other.  Row r belongs to the
+ * sequence i with offsets[i] <= r < offsets[i+1]; without offsets all rows are one sequence.  A row COUNTS when tokens[r] >= 0 (where
+ * tokens are given), mask[r] != 0 (where a mask is given) and, for the losses, it belongs to a sequence.  What a row that does not count holds is
+ * never used, NaN included: its outputs are zeros.  A token >= vocab gives NaN.  Logits of -inf are tokens without probability; a row of
+ * nothing else has logp -inf, entropy 0 and a gradient of zeros.  NaN or +inf among a row's logits gives NaN.
+ * Offsets that do not ascend, or pass [0, rows], are an error of the caller's that the kernels answer with wrong numbers, within bounds.
+ */
+enum { ANAKIN_DTYPE_F32 = 0, ANAKIN_DTYPE_BF16 = 1, ANAKIN_DTYPE_F16 = 2 };
+
+/* Plain-old-data description of the rows.  struct_size must be sizeof(anakin_token_rows). */
+typedef struct anakin_token_rows {
+    uint32_t struct_size;
+    int32_t dtype;         /* ANAKIN_DTYPE_* of the logits and their gradient */
+    int64_t rows;          /* >= 0, < 2^31 */
+    int64_t vocab;         /* >= 1, < 2^31 */
+    int64_t ld;            /* elements from one row of the logits to the next, >= vocab (no alignment needed) */
+    const void* logits;    /* [rows][ld] */
+    const void* tokens;    /* [rows], token_bytes each; < 0: the row does not count */
+    const uint8_t* mask;   /* [rows] or NULL */
+    const void* offsets;   /* [sequences + 1], offset_bytes each, ascending; or NULL */
+    int64_t sequences;     /* >= 0, < 2^31 */
+    int32_t token_bytes;   /* 4 or 8: int32 or int64 */
+    int32_t offset_bytes;  /* 4 or 8 */
+    float scale;           /* the distribution is softmax(scale * logits): one over the sampling temperature; > 0 */
+    uint32_t reserved;     /* 0 */
+} anakin_token_rows;
+
+enum { ANAKIN_KL_NONE = 0, ANAKIN_KL_1 = 1, ANAKIN_KL_2 = 2, ANAKIN_KL_3 = 3 };
+enum { ANAKIN_MEAN_TOKEN = 0, ANAKIN_MEAN_SEQUENCE = 1, ANAKIN_MEAN_FIXED = 2 };
+
+/*
+ * The clipped surrogate with a KL term.  With l = log pi(token), r = exp(l - old), A the advantage, the loss is the sum over counted rows of
+ *   w ( pg + kl_coef kl - entropy_coef H ),
+ *   pg = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A); where A < 0 and dual_clip > 0, at most -dual_clip A,
+ *   kl = 0 | z | z^2/2 | exp(-z) - 1 + z,  z = l - ref  (the three usual one-sample estimates of KL(pi, ref); their own gradients are taken),
+ *   w  = 1/(counted rows) | 1/(sequences with a counted row * counted rows of this one) | 1/divisor.
+ * Differences l - old and l - ref are bounded to +-80 before exp.  At r equal to a bound the gradient passes.  A = 0 gives pg = 0.
+ */
+typedef struct anakin_policy_objective {
+    uint32_t struct_size;  /* sizeof(anakin_policy_objective) */
+    float clip_low;        /* [0, 1] */
+    float clip_high;       /* >= 0 */
+    float dual_clip;       /* 0 (off) or >= 1 */
+    int32_t kl;            /* ANAKIN_KL_* */
+    float kl_coef;
+    float entropy_coef;
+    int32_t mean;          /* ANAKIN_MEAN_* */
+    float divisor;         /* > 0 with ANAKIN_MEAN_FIXED */
+} anakin_policy_objective;
+#define ANAKIN_POLICY_STATS 6  /* loss, sum w pg, sum w kl, sum w H, sum w [gradient of pg cut off by a clip], sum w (old - l) */
+
+enum { ANAKIN_PREFER_SIGMOID = 0, ANAKIN_PREFER_HINGE = 1, ANAKIN_PREFER_SQUARED = 2 };
+
+/*
+ * The preference loss over pairs.  Of 2P sequences, i < P is an answer that was preferred to sequence P + i.  With a = the sum (mean = 1: the
+ * mean) of l - ref over a sequence's counted rows (ref = 0 where none is given) and z = beta (a_i - a_{P+i}) - margin:
+ *   sigmoid  -(1 - smoothing) log sigmoid(z) - smoothing log sigmoid(-z);   hinge  max(0, 1 - z);   squared  ((z - 1/2) / beta)^2
+ * averaged over the pairs both of whose sequences have a counted row; the others carry no loss.
+ */
+typedef struct anakin_preference_objective {
+    uint32_t struct_size;  /* sizeof(anakin_preference_objective) */
+    int32_t kind;          /* ANAKIN_PREFER_* */
+    float beta;            /* > 0 */
+    float margin;
+    float smoothing;       /* [0, 0.5]; used by sigmoid only */
+    int32_t mean;          /* 0 or 1 */
+} anakin_preference_objective;
+#define ANAKIN_PREFERENCE_STATS 5  /* loss, share of pairs with z > 0, mean beta a of the preferred, of the others, mean z */
+
+/*
+ * Log-probability of every row's token, and the entropy of its distribution.
+ *   out  logp f32[rows]; entropy f32[rows] or NULL; norm f32[rows][2] or NULL: the largest logit m and log sum exp(scale (x - m)), which
+ *        the gradient needs (the row's log-sum-exp is scale m + the second)
+ * No workspace.  Offsets are not looked at.
+ */
+int anakin_token_logp(const anakin_token_rows* rows, float* logp, float* entropy, float* norm, void* cuda_stream);
+
+/*
+ * Gradient of the logits from the gradients of logp and entropy:
+ *   dlogits_j = scale ( dlogp ([j = token] - p_j) - dentropy p_j (log p_j + H) )
+ * norm and entropy are what anakin_token_logp wrote for the same rows; dentropy and entropy may both be NULL.  dlogits [rows][ld_out] may be
+ * the logits themselves (with ld_out = ld); otherwise they must not overlap.  Columns from vocab on are left as they are.
+ */
+int anakin_token_logp_backward(const anakin_token_rows* rows, const float* norm, const float* entropy, const float* dlogp,
+                               const float* dentropy, void* dlogits, int64_t ld_out, void* cuda_stream);
+
+/* Workspace of the three losses below for this many rows and sequences (at least 256-byte aligned, like every workspace). */
+int anakin_token_workspace_bytes(int64_t rows, int64_t sequences, size_t* bytes);
+
+/*
+ * The clipped loss from log-probabilities (rows->logits is not looked at; tokens may be NULL).
+ *   in   logp, adv f32[rows]; old_logp f32[rows] or NULL (then r = 1: the first step on a rollout of the same policy); ref_logp f32[rows],
+ *        needed with a KL term; entropy f32[rows] or NULL (the term is then left out)
+ *   out  stats f32[ANAKIN_POLICY_STATS]; dlogp f32[rows]; dentropy f32[rows] or NULL
+ */
+int anakin_token_policy_loss(const anakin_token_rows* rows, const anakin_policy_objective* objective, const float* logp, const float* old_logp,
+                             const float* adv, const float* ref_logp, const float* entropy, float* stats, float* dlogp, float* dentropy,
+                             void* dev_workspace, size_t bytes, void* cuda_stream);
+
+/*
+ * The clipped loss from logits, with the gradient of the logits, in one pass over them: equal to anakin_token_logp,
+ * anakin_token_policy_loss and anakin_token_logp_backward in a row.  logp and entropy (f32[rows]) may be NULL.  dlogits as in
+ * anakin_token_logp_backward.
+ */
+int anakin_token_policy_grad(const anakin_token_rows* rows, const anakin_policy_objective* objective, const float* old_logp, const float* adv,
+                             const float* ref_logp, float* stats, float* logp, float* entropy, void* dlogits, int64_t ld_out,
+                             void* dev_workspace, size_t bytes, void* cuda_stream);
+
+/*
+ * The preference loss from log-probabilities; rows->sequences = 2P, offsets are needed, rows->logits is not looked at, tokens may be NULL.
+ *   in   logp f32[rows]; ref_logp f32[rows] or NULL
+ *   out  stats f32[ANAKIN_PREFERENCE_STATS]; margin f32[P] (z; 0 for a pair that carries no loss); dlogp f32[rows]
+ */
+int anakin_token_preference_loss(const anakin_token_rows* rows, const anakin_preference_objective* objective, const float* logp,
+                                 const float* ref_logp, float* stats, float* margin, float* dlogp, void* dev_workspace, size_t bytes,
+                                 void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits.  (The paper has no counterpart.)  A backward pass reads the activations that the forward pass kept; these
+ * calls keep a matrix x [rows][cols] in 8 bits a value and 8 more for every 32, and read it where the backward pass needs it.  Conventions
+ * as above.
+ *
+ * Format (what OCP's microscaling specification calls MXFP8 with e4m3 elements; the scale is rounded up, so that nothing saturates): every
+ * row in blocks of 32 columns; a block is e4m3 numbers (1 sign, 4 exponent, 3 fraction bits, up to 448) times 2^(scale - 127), the smallest power
+ * of two that brings the block's largest value within 448, from 2^-117 to 2^120 (there values stop at 240).  Each value is rounded to nearest, ties to
+ * even: off by at most 2^-4 of itself, or, far below the block's largest, 2^-10 times the scale.  NaN and infinities come back as NaN and do not count for the scale.
+ *   codes  u8[rows][cols rounded up to 32], zeros behind the columns;   scales  u8[rows][blocks].  codes 16-byte aligned.
+ */
+enum { ANAKIN_ACT_IDENTITY = 0, ANAKIN_ACT_RELU = 1, ANAKIN_ACT_SILU = 2, ANAKIN_ACT_GELU = 3 };  /* GELU: x times the normal distribution function */
+
+/* Sizes of the two arrays of a checkpoint. */
+int anakin_ckpt_bytes(int64_t rows, int64_t cols, size_t* code_bytes, size_t* scale_bytes);
+
+/* y = act(x) and the checkpoint of x in one pass over x; y (dtype of x) may be NULL, or x itself. */
+int anakin_ckpt_forward(int dtype, int act, int64_t rows, int64_t cols, const void* x, int64_t ldx, void* y, int64_t ldy, uint8_t* codes,
+                        uint8_t* scales, void* cuda_stream);
+
+/* The kept values as a matrix of `dtype` (values past an fp16's largest stop there). */
+int anakin_ckpt_unpack(int dtype, int64_t rows, int64_t cols, const uint8_t* codes, const uint8_t* scales, void* x, int64_t ldx, void* cuda_stream);
+
+/* dx = dy act'(x) with x from its checkpoint; dx may be dy itself. */
+int anakin_ckpt_backward(int dtype, int act, int64_t rows, int64_t cols, const uint8_t* codes, const uint8_t* scales, const void* dy,
+                         int64_t lddy, void* dx, int64_t lddx, void* cuda_stream);
+
+/*
+ * Weight gradient of a layer whose input is act(x): dw[cols][n] (+)= act(x)^T dy, x from its checkpoint, dy [rows][n] of `dtype`; fp32 sums.
+ * act: identity or relu (their values are exact in the tensor cores' 16 bits; others are refused with ANAKIN_E_UNSUPPORTED_CFG: checkpoint the
+ * activation's output instead).  accumulate != 0 adds to dw (micro-batches).  rows = 0 gives zeros.
+ * Every wait inside is bounded; one that gives up sets the bit that anakin_status documents in *dev_status (i32, may be NULL; the caller zeroes it).
+ */
+int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t n, size_t* bytes);
+int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int64_t n, const uint8_t* codes, const uint8_t* scales,
+                            const void* dy, int64_t lddy, float* dw, int64_t lddw, int accumulate, void* dev_workspace, size_t bytes,
+                            int32_t* dev_status, void* cuda_stream);
+
 /* Static description of an error code. */
 const char* anakin_strerror(int code);
 

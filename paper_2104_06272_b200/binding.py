@@ -50,6 +50,10 @@ EXPORTS = [
     "anakin_blob_bytes", "anakin_status", "anakin_launch_count", "anakin_strerror", "anakin_last_cuda_error",
     "anakin_profile_enable", "anakin_profile_read", "anakin_kernel_count", "anakin_kernel_name",
     "anakin_rollout_noalloc", "anakin_noalloc_status", "anakin_selftest_wait_timeout",
+    # policies over token vocabularies and activation checkpoints: Python functions in tokens.py
+    "anakin_token_logp", "anakin_token_logp_backward", "anakin_token_workspace_bytes", "anakin_token_policy_loss", "anakin_token_policy_grad",
+    "anakin_token_preference_loss", "anakin_ckpt_bytes", "anakin_ckpt_forward", "anakin_ckpt_unpack", "anakin_ckpt_backward",
+    "anakin_ckpt_weight_grad_workspace_bytes", "anakin_ckpt_weight_grad",
 ]
 
 _vp = C.c_void_p

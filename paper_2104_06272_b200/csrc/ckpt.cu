@@ -1,0 +1,300 @@
+// Activation checkpoints in 8 bits: every row in blocks of 32 columns, a block as e4m3 numbers times a power of two.
+//
+// scale exponent E = the smallest with top 2^-E <= 448, top the block's largest finite |x|; code = round(x 2^-E) to e4m3, ties to even.  Scaling by
+// a power of two is exact, so the code is the only rounding.  Everything here is bound by memory: a thread moves 8 columns of a row (one 16-byte
+// load of 16-bit elements, 8 code bytes), four neighbours share a block, and a thread has two such pieces in flight.
+#include <cuda_fp8.h>
+
+#include "ckpt.cuh"
+#include "token_rows.cuh"
+
+namespace anakin {
+namespace ckpt {
+namespace {
+
+using tok::from_f;
+using tok::to_f;
+
+// n / d and n % d for n < 2^31 by a multiplication (d >= 1; Granlund and Montgomery 1994): q = (n mul) >> (32 + shift).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    explicit FastDiv(uint32_t div = 1) : d(div) {
+        shift = 0;
+        while ((1ull << shift) < div) ++shift;
+        // ceil(2^(31 + shift) / d) < 2^32, error below 2^shift: exact for n < 2^31
+        mul = (uint32_t)(((1ull << (31 + shift)) + div - 1) / div);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (uint32_t)(((unsigned long long)n * mul) >> (31 + shift)); }
+};
+
+struct Args {
+    long long rows;  // of this launch
+    int cols, blocks;
+    FastDiv per_row;  // pieces of 8 columns in a row (4 a block)
+    uint32_t pieces;  // rows * per_row < 2^31
+    const void* x;    // forward: x; backward: dy
+    long long ldx;
+    void* y;          // forward: act(x) or null; unpack: x; backward: dx
+    long long ldy;
+    uint8_t* codes;
+    uint8_t* scales;
+    bool vec_x, vec_y;  // every row starts on a 16-byte boundary
+};
+
+template <int ACT> __device__ __forceinline__ float act_of(float x) {
+    if (ACT == ANAKIN_ACT_RELU) return x > 0.f ? x : x != x ? x : 0.f;
+    if (ACT == ANAKIN_ACT_SILU) return x / (1.f + expf(-x));
+    if (ACT == ANAKIN_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
+    return x;
+}
+template <int ACT> __device__ __forceinline__ float slope_of(float x) {
+    if (ACT == ANAKIN_ACT_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
+    if (ACT == ANAKIN_ACT_SILU) {
+        const float g = 1.f / (1.f + expf(-x));
+        return g * (1.f + x * (1.f - g));
+    }
+    if (ACT == ANAKIN_ACT_GELU) return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * 0.39894228040143268f * expf(-0.5f * x * x);
+    return 1.f;
+}
+
+// Eight columns of a row from column j on; what lies behind the row reads as zeros.
+template <class T> __device__ __forceinline__ void load8(const T* row, int j, int cols, bool vec, float (&f)[8]) {
+    if (vec && j + 8 <= cols) {
+        const uint4* p = reinterpret_cast<const uint4*>(row + j);
+        if constexpr (sizeof(T) == 4) {
+            const uint4 a = p[0], b = p[1];
+            f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+            f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+        } else {
+            tok::unpack16(p[0], f, (const T*)nullptr);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = j + i < cols ? to_f(row[j + i]) : 0.f;
+}
+template <class T> __device__ __forceinline__ void store8(T* row, int j, int cols, bool vec, const float (&f)[8]) {
+    if (vec && j + 8 <= cols) {
+        uint4* p = reinterpret_cast<uint4*>(row + j);
+        if constexpr (sizeof(T) == 4) {
+            p[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+            p[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+        } else {
+            p[0] = tok::pack16(f, (const T*)nullptr);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (j + i < cols) row[j + i] = from_f<T>(f[i]);
+}
+
+// The smallest E in [-117, 120] with top 2^-E <= 448 = 1.75 2^8, from the bits of top (finite, >= 0).
+__device__ __forceinline__ int exponent_of(float top) {
+    const uint32_t u = __float_as_uint(top);
+    const int e = (int)(u >> 23) - 127;  // (zero and subnormals: -127, below every limit)
+    const int E = e - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return E < kMinExp ? kMinExp : E;  // (never above 120: e <= 127)
+}
+
+template <class T, int ACT>
+__global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
+    pdl_wait();
+    constexpr int U = 2;
+    // (a warp's lanes stay together: four of them share a block's largest value; `pieces` is a multiple of 4)
+    for (uint32_t p0 = blockIdx.x * 256u * U + (threadIdx.x & ~31u); p0 < a.pieces; p0 += gridDim.x * 256u * U) {
+        float f[U][8];
+        uint32_t r[U], j[U];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t p = p0 + 256u * u + (threadIdx.x & 31);
+            in[u] = p < a.pieces;
+            r[u] = a.per_row.div(in[u] ? p : 0u);
+            j[u] = ((in[u] ? p : 0u) - r[u] * a.per_row.d) * 8;
+            if (in[u]) load8(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, j[u], a.cols, a.vec_x, f[u]);
+            else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[u][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = fabsf(f[u][i]);
+                top = fmaxf(top, v < INFINITY ? v : 0.f);
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            if (!in[u]) continue;
+            const int E = exponent_of(top);
+            const float down = __uint_as_float((uint32_t)(127 - E) << 23);  // 2^-E: E in [-117, 120]
+            uint32_t w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t c = 0;
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const float x0 = f[u][4 * h + i], x1 = f[u][4 * h + i + 1];
+                    float v0 = x0 * down, v1 = x1 * down;
+                    if (E == kMaxExp) {  // (256 times 2^120 would be past the largest fp32 number)
+                        v0 = v0 > 240.f ? 240.f : v0 < -240.f ? -240.f : v0;
+                        v1 = v1 > 240.f ? 240.f : v1 < -240.f ? -240.f : v1;
+                    }
+                    uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(v0, v1), __NV_SATFINITE, __NV_E4M3);
+                    if (!(fabsf(x0) < INFINITY)) b = (b & 0xFF00u) | 0x7Fu;
+                    if (!(fabsf(x1) < INFINITY)) b = (b & 0x00FFu) | 0x7F00u;
+                    c |= b << (8 * i);
+                }
+                w[h] = c;
+            }
+            *reinterpret_cast<uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]) = make_uint2(w[0], w[1]);
+            if ((threadIdx.x & 3) == 0) a.scales[(size_t)r[u] * a.blocks + j[u] / 32] = (uint8_t)(E + 127);
+            if (a.y) {
+                float g[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] = act_of<ACT>(f[u][i]);
+                store8(static_cast<T*>(a.y) + (long long)r[u] * a.ldy, j[u], a.cols, a.vec_y, g);
+            }
+        }
+    }
+}
+
+template <class T> __device__ __forceinline__ float within(float v) { return v; }
+template <> __device__ __forceinline__ float within<__half>(float v) { return v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v; }
+
+// Unpack (BACK = false): y = the kept values; BACK: y = x act'(kept).
+template <class T, int ACT, bool BACK>
+__global__ void __launch_bounds__(256) k_ckpt_read(Args a) {
+    pdl_wait();
+    constexpr int U = 2;
+    for (uint32_t p0 = blockIdx.x * 256u * U + threadIdx.x; p0 < a.pieces; p0 += gridDim.x * 256u * U) {
+        uint2 c[U];
+        float d[U][8];
+        uint32_t r[U], j[U], s[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t p = p0 + 256u * u;
+            if (p >= a.pieces) continue;
+            r[u] = a.per_row.div(p);
+            j[u] = (p - r[u] * a.per_row.d) * 8;
+            c[u] = *reinterpret_cast<const uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]);
+            s[u] = a.scales[(size_t)r[u] * a.blocks + j[u] / 32];
+            if (BACK) load8(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, j[u], a.cols, a.vec_x, d[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p0 + 256u * u >= a.pieces) continue;
+            float v[8];
+            decode8(c[u], s[u], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = BACK ? d[u][i] * slope_of<ACT>(v[i]) : within<T>(v[i]);
+            store8(static_cast<T*>(a.y) + (long long)r[u] * a.ldy, j[u], a.cols, a.vec_y, v);
+        }
+    }
+}
+
+enum { FORWARD = 0, UNPACK = 1, BACKWARD = 2 };
+
+template <class T, int ACT, int MODE>
+cudaError_t launch_one(const Args& a, cudaStream_t s) {
+    const uint32_t n = (a.pieces + 511) / 512;
+    const dim3 grid(n < 148u * 32 ? n : 148u * 32);
+    if constexpr (MODE == FORWARD) return launch<k_ckpt_forward<T, ACT>>(grid, dim3(256), 0, s, a);
+    else return launch<k_ckpt_read<T, ACT, MODE == BACKWARD>>(grid, dim3(256), 0, s, a);
+}
+template <class T, int MODE>
+cudaError_t launch_act(int act, const Args& a, cudaStream_t s) {
+    if constexpr (MODE == UNPACK) return launch_one<T, ANAKIN_ACT_IDENTITY, MODE>(a, s);
+    else switch (act) {
+        case ANAKIN_ACT_RELU: return launch_one<T, ANAKIN_ACT_RELU, MODE>(a, s);
+        case ANAKIN_ACT_SILU: return launch_one<T, ANAKIN_ACT_SILU, MODE>(a, s);
+        case ANAKIN_ACT_GELU: return launch_one<T, ANAKIN_ACT_GELU, MODE>(a, s);
+        default: return launch_one<T, ANAKIN_ACT_IDENTITY, MODE>(a, s);
+    }
+}
+
+// A launch covers fewer than 2^31 pieces; a larger matrix takes several, each a range of rows.
+template <int MODE>
+int run(int dtype, int act, long long rows, long long cols, const void* x, long long ldx, void* y, long long ldy, uint8_t* codes, uint8_t* scales,
+        cudaStream_t s) {
+    const size_t es = dtype == ANAKIN_DTYPE_F32 ? 4 : 2;
+    Args a;
+    a.cols = (int)cols;
+    a.blocks = (int)((cols + 31) / 32);
+    a.per_row = FastDiv((uint32_t)a.blocks * 4);
+    a.vec_x = ((uintptr_t)x & 15) == 0 && ldx * es % 16 == 0;
+    a.vec_y = ((uintptr_t)y & 15) == 0 && ldy * es % 16 == 0;
+    // (the last CTA's pieces, and a step of the whole grid, stay below 2^32)
+    const long long most = ((1ll << 31) - 1) / ((long long)a.blocks * 4);
+    for (long long r0 = 0; r0 < rows; r0 += most) {
+        const long long n = rows - r0 < most ? rows - r0 : most;
+        a.rows = n;
+        a.pieces = (uint32_t)(n * a.blocks * 4);
+        a.x = static_cast<const unsigned char*>(x) + (x ? (size_t)r0 * ldx * es : 0);
+        a.ldx = ldx;
+        a.y = y ? static_cast<unsigned char*>(y) + (size_t)r0 * ldy * es : nullptr;
+        a.ldy = ldy;
+        a.codes = codes + (size_t)r0 * a.blocks * 32;
+        a.scales = scales + (size_t)r0 * a.blocks;
+        const cudaError_t e = dtype == ANAKIN_DTYPE_F32 ? launch_act<float, MODE>(act, a, s)
+                              : dtype == ANAKIN_DTYPE_BF16 ? launch_act<__nv_bfloat16, MODE>(act, a, s) : launch_act<__half, MODE>(act, a, s);
+        if (e != cudaSuccess) return tok::fail();
+    }
+    return ANAKIN_OK;
+}
+
+}  // namespace
+
+int check(int dtype, int act, int64_t rows, int64_t cols, const uint8_t* codes, const uint8_t* scales) {
+    if (dtype < ANAKIN_DTYPE_F32 || dtype > ANAKIN_DTYPE_F16 || act < ANAKIN_ACT_IDENTITY || act > ANAKIN_ACT_GELU) return ANAKIN_E_INVALID_ARG;
+    if (rows < 0 || cols < 1 || rows >= (int64_t(1) << 31) || cols > (int64_t(1) << 28)) return ANAKIN_E_INVALID_ARG;
+    if (rows > 0 && (!codes || !scales || ((uintptr_t)codes & 15))) return ANAKIN_E_INVALID_ARG;
+    return ANAKIN_OK;
+}
+
+}  // namespace ckpt
+}  // namespace anakin
+
+using namespace anakin;
+
+static bool bad_matrix(int dtype, int64_t rows, int64_t cols, const void* p, int64_t ld) {
+    return rows > 0 && (!p || ((uintptr_t)p & (dtype == ANAKIN_DTYPE_F32 ? 3 : 1)) || ld < cols || ld >= (int64_t(1) << 40));
+}
+
+extern "C" {
+
+int anakin_ckpt_bytes(int64_t rows, int64_t cols, size_t* code_bytes, size_t* scale_bytes) {
+    if (!code_bytes || !scale_bytes || rows < 0 || cols < 1 || rows >= (int64_t(1) << 31) || cols > (int64_t(1) << 28)) return ANAKIN_E_INVALID_ARG;
+    const size_t blocks = (size_t)((cols + 31) / 32);
+    *code_bytes = (size_t)rows * blocks * 32;
+    *scale_bytes = (size_t)rows * blocks;
+    return ANAKIN_OK;
+}
+
+int anakin_ckpt_forward(int dtype, int act, int64_t rows, int64_t cols, const void* x, int64_t ldx, void* y, int64_t ldy, uint8_t* codes,
+                        uint8_t* scales, void* cuda_stream) {
+    const int rc = ckpt::check(dtype, act, rows, cols, codes, scales);
+    if (rc != ANAKIN_OK) return rc;
+    if (bad_matrix(dtype, rows, cols, x, ldx) || (y && bad_matrix(dtype, rows, cols, y, ldy))) return ANAKIN_E_INVALID_ARG;
+    return ckpt::run<ckpt::FORWARD>(dtype, act, rows, cols, x, ldx, y, ldy, codes, scales, (cudaStream_t)cuda_stream);
+}
+
+int anakin_ckpt_unpack(int dtype, int64_t rows, int64_t cols, const uint8_t* codes, const uint8_t* scales, void* x, int64_t ldx, void* cuda_stream) {
+    const int rc = ckpt::check(dtype, ANAKIN_ACT_IDENTITY, rows, cols, codes, scales);
+    if (rc != ANAKIN_OK) return rc;
+    if (bad_matrix(dtype, rows, cols, x, ldx)) return ANAKIN_E_INVALID_ARG;
+    return ckpt::run<ckpt::UNPACK>(dtype, 0, rows, cols, nullptr, 0, x, ldx, const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), (cudaStream_t)cuda_stream);
+}
+
+int anakin_ckpt_backward(int dtype, int act, int64_t rows, int64_t cols, const uint8_t* codes, const uint8_t* scales, const void* dy,
+                         int64_t lddy, void* dx, int64_t lddx, void* cuda_stream) {
+    const int rc = ckpt::check(dtype, act, rows, cols, codes, scales);
+    if (rc != ANAKIN_OK) return rc;
+    if (bad_matrix(dtype, rows, cols, dy, lddy) || bad_matrix(dtype, rows, cols, dx, lddx)) return ANAKIN_E_INVALID_ARG;
+    return ckpt::run<ckpt::BACKWARD>(dtype, act, rows, cols, dy, lddy, dx, lddx, const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

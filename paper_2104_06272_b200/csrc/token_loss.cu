@@ -1,0 +1,423 @@
+// The losses over tokens from log-probabilities: the clipped policy loss with a KL term, and the preference loss over pairs of answers; and the
+// counts of rows that their means divide by.  All of it is a few vectors of one number a token: the launches cost more than the
+// bytes up to some hundred thousand tokens, so short batches are done by one CTA in one launch.
+#include "token_rows.cuh"
+
+namespace anakin {
+namespace tok {
+
+int fail() {
+    cudaGetLastError();
+    return ANAKIN_E_CUDA;
+}
+
+int check_rows(const anakin_token_rows* p, bool need_logits, bool need_tokens, bool need_offsets, Rows* q) {
+    if (!p || p->struct_size != sizeof(anakin_token_rows) || p->reserved != 0) return ANAKIN_E_INVALID_ARG;
+    constexpr int64_t LIMIT = int64_t(1) << 31;
+    if (p->rows < 0 || p->rows >= LIMIT || p->sequences < 0 || p->sequences >= LIMIT - 1) return ANAKIN_E_INVALID_ARG;
+    if (p->tokens && p->token_bytes != 4 && p->token_bytes != 8) return ANAKIN_E_INVALID_ARG;
+    if (p->offsets && p->offset_bytes != 4 && p->offset_bytes != 8) return ANAKIN_E_INVALID_ARG;
+    if (p->tokens && ((uintptr_t)p->tokens & (p->token_bytes - 1))) return ANAKIN_E_INVALID_ARG;
+    if (p->offsets && ((uintptr_t)p->offsets & (p->offset_bytes - 1))) return ANAKIN_E_INVALID_ARG;
+    if (need_offsets && !p->offsets) return ANAKIN_E_INVALID_ARG;
+    if (need_logits) {
+        if (p->dtype < ANAKIN_DTYPE_F32 || p->dtype > ANAKIN_DTYPE_F16) return ANAKIN_E_INVALID_ARG;
+        if (p->vocab < 1 || p->vocab >= LIMIT || p->ld < p->vocab || !(p->scale > 0.f) || !(p->scale < INFINITY)) return ANAKIN_E_INVALID_ARG;
+        if (p->rows > 0 && (!p->logits || ((uintptr_t)p->logits & (p->dtype == ANAKIN_DTYPE_F32 ? 3 : 1)))) return ANAKIN_E_INVALID_ARG;
+    }
+    if (need_tokens && p->rows > 0 && !p->tokens) return ANAKIN_E_INVALID_ARG;
+    q->rows = p->rows; q->vocab = p->vocab; q->ld = p->ld;
+    q->logits = p->logits; q->tokens = p->tokens; q->mask = p->mask; q->offsets = p->offsets;
+    q->sequences = p->offsets ? (int)p->sequences : 1;
+    q->token_bytes = p->token_bytes; q->offset_bytes = p->offset_bytes;
+    q->scale = p->scale;
+    return ANAKIN_OK;
+}
+
+int check_policy(const anakin_policy_objective* p, Objective* o) {
+    if (!p || p->struct_size != sizeof(anakin_policy_objective)) return ANAKIN_E_INVALID_ARG;
+    if (!(p->clip_low >= 0.f && p->clip_low <= 1.f) || !(p->clip_high >= 0.f) || !(p->dual_clip == 0.f || p->dual_clip >= 1.f)) return ANAKIN_E_INVALID_ARG;
+    if (p->kl < ANAKIN_KL_NONE || p->kl > ANAKIN_KL_3 || p->mean < ANAKIN_MEAN_TOKEN || p->mean > ANAKIN_MEAN_FIXED) return ANAKIN_E_INVALID_ARG;
+    if (p->mean == ANAKIN_MEAN_FIXED && !(p->divisor > 0.f)) return ANAKIN_E_INVALID_ARG;
+    if (p->kl_coef != p->kl_coef || p->entropy_coef != p->entropy_coef) return ANAKIN_E_INVALID_ARG;
+    o->lo = 1.f - p->clip_low;
+    o->hi = 1.f + p->clip_high;
+    o->dual = p->dual_clip;
+    o->kl = p->kl;
+    o->kl_coef = p->kl == ANAKIN_KL_NONE ? 0.f : p->kl_coef;
+    o->entropy_coef = p->entropy_coef;
+    o->mean = p->mean;
+    o->inv_divisor = p->mean == ANAKIN_MEAN_FIXED ? 1.f / p->divisor : 0.f;
+    return ANAKIN_OK;
+}
+
+Workspace carve(void* base, long long sequences) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) { void* p = static_cast<unsigned char*>(base) + off; off += (bytes + 255) / 256 * 256; return p; };
+    Workspace w;
+    w.counts = static_cast<Counts*>(take(sizeof(Counts)));
+    w.part = static_cast<double*>(take(sizeof(double) * kMaxPartials * kPolicyParts));
+    w.per_seq = static_cast<int*>(take(sizeof(int) * (size_t)sequences));
+    w.sums = static_cast<double*>(take(sizeof(double) * (size_t)sequences));
+    w.bytes = off;
+    return w;
+}
+
+namespace {
+
+constexpr int kSmallRows = 8192, kSmallSeqs = 4096;  // up to here one CTA does it all
+
+// Adds a warp's 32 rows to the counts: lanes whose rows lie in one sequence add once.  Sums of integers: any order gives the same.
+__device__ __forceinline__ void add_counts(bool counts, int seq, unsigned long long* rows, unsigned long long* seqs, int* per_seq) {
+    const unsigned in = __ballot_sync(0xFFFFFFFFu, counts);
+    if (!in) return;
+    const int lane = threadIdx.x & 31;
+    if (lane == __ffs(in) - 1) atomicAdd(rows, (unsigned long long)__popc(in));
+    if (!per_seq || !counts) return;
+    const unsigned same = __match_any_sync(in, seq);
+    if (lane == __ffs(same) - 1 && atomicAdd(&per_seq[seq], __popc(same)) == 0) atomicAdd(seqs, 1ull);
+}
+
+__global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* per_seq) {
+    PDL_START();
+    const long long stride = (long long)gridDim.x * 256;
+    for (long long r0 = (long long)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < q.rows; r0 += stride) {
+        const long long r = r0 + (threadIdx.x & 31);
+        bool counts = r < q.rows && row_counts(q, r);
+        int seq = 0;
+        if (counts) {
+            seq = sequence_of(q, r);
+            counts = seq >= 0 && seq < q.sequences;
+        }
+        add_counts(counts, seq, &c->rows, &c->sequences, per_seq);
+    }
+}
+
+__global__ void __launch_bounds__(256) k_policy_stats(const double* part, int n, Objective o, float* stats) {
+    PDL_START();
+    __shared__ double red[8];
+    double v[kPolicyParts] = {0.0, 0.0, 0.0, 0.0, 0.0};
+    for (int i = threadIdx.x; i < n; i += 256)
+        for (int k = 0; k < kPolicyParts; ++k) v[k] += part[(size_t)i * kPolicyParts + k];
+    for (int k = 0; k < kPolicyParts; ++k) v[k] = block_sum(v[k], red);
+    if (threadIdx.x == 0) {
+        stats[0] = (float)(v[0] + (double)o.kl_coef * v[1] - (double)o.entropy_coef * v[2]);
+        for (int k = 0; k < kPolicyParts; ++k) stats[1 + k] = (float)v[k];
+    }
+}
+
+struct PolicyArgs2 {
+    Rows q;
+    Objective o;
+    const float* logp;
+    const float* old_logp;
+    const float* adv;
+    const float* ref;
+    const float* entropy;
+    float* stats;
+    float* dlogp;
+    float* dentropy;
+    Counts* counts;
+    int* per_seq;
+    double* part;
+};
+
+__device__ __forceinline__ void policy_row(const PolicyArgs2& A, long long r, const Counts* c, const int* per_seq, double (&part)[kPolicyParts]) {
+    const Rows& q = A.q;
+    bool counts = row_counts(q, r);
+    int seq = 0;
+    if (counts) {
+        seq = sequence_of(q, r);
+        counts = seq >= 0 && seq < q.sequences;
+    }
+    float g = 0.f, h = 0.f;
+    if (counts) {
+        const PolicyTerms p = policy_terms(A.o, A.logp[r], A.old_logp ? A.old_logp[r] : 0.f, A.old_logp != nullptr, A.adv[r], A.ref ? A.ref[r] : 0.f);
+        const float w = row_weight(A.o, c, per_seq, seq);
+        const float H = A.entropy ? A.entropy[r] : 0.f;
+        part[0] += (double)(w * p.pg); part[1] += (double)(w * p.kl); part[2] += (double)(w * H);
+        part[3] += (double)(w * p.cut); part[4] += (double)(w * p.old_minus_new);
+        g = w * p.dlogp;
+        h = A.entropy ? -A.o.entropy_coef * w : 0.f;
+    }
+    A.dlogp[r] = g;
+    if (A.dentropy) A.dentropy[r] = h;
+}
+
+__global__ void __launch_bounds__(256) k_policy_loss(PolicyArgs2 A) {
+    PDL_START();
+    __shared__ double red[8];
+    double part[kPolicyParts] = {0.0, 0.0, 0.0, 0.0, 0.0};
+    for (long long r = (long long)blockIdx.x * 256 + threadIdx.x; r < A.q.rows; r += (long long)gridDim.x * 256) policy_row(A, r, A.counts, A.per_seq, part);
+    for (int k = 0; k < kPolicyParts; ++k) {
+        const double s = block_sum(part[k], red);
+        if (threadIdx.x == 0) A.part[(size_t)blockIdx.x * kPolicyParts + k] = s;
+    }
+}
+
+// One CTA: counts, terms and statistics of up to kSmallRows rows and kSmallSeqs sequences.
+__global__ void __launch_bounds__(1024) k_policy_loss_small(PolicyArgs2 A) {
+    PDL_START();
+    __shared__ double red[32];
+    __shared__ Counts c;
+    __shared__ int per_seq[kSmallSeqs];
+    const Rows& q = A.q;
+    if (A.o.mean != ANAKIN_MEAN_FIXED) {
+        const bool by_seq = A.o.mean == ANAKIN_MEAN_SEQUENCE;
+        if (threadIdx.x == 0) c = Counts{0ull, 0ull};
+        if (by_seq) for (int i = threadIdx.x; i < q.sequences; i += 1024) per_seq[i] = 0;
+        __syncthreads();
+        for (int r0 = threadIdx.x & ~31; r0 < (int)q.rows; r0 += 1024) {
+            const int r = r0 + (threadIdx.x & 31);
+            bool counts = r < (int)q.rows && row_counts(q, r);
+            int seq = 0;
+            if (counts) {
+                seq = sequence_of(q, r);
+                counts = seq >= 0 && seq < q.sequences;
+            }
+            add_counts(counts, seq, &c.rows, &c.sequences, by_seq ? per_seq : nullptr);
+        }
+        __syncthreads();
+    }
+    double part[kPolicyParts] = {0.0, 0.0, 0.0, 0.0, 0.0};
+    for (int r = threadIdx.x; r < (int)q.rows; r += 1024) policy_row(A, r, &c, per_seq, part);
+    for (int k = 0; k < kPolicyParts; ++k) part[k] = block_sum(part[k], red);
+    if (threadIdx.x == 0) {
+        A.stats[0] = (float)(part[0] + (double)A.o.kl_coef * part[1] - (double)A.o.entropy_coef * part[2]);
+        for (int k = 0; k < kPolicyParts; ++k) A.stats[1 + k] = (float)part[k];
+    }
+}
+
+// ---- preference loss ----
+struct PreferArgs {
+    Rows q;
+    int P, kind, mean;
+    float beta, margin, smoothing;
+    const float* logp;
+    const float* ref;
+    float* stats;
+    float* zout;
+    float* dlogp;
+    int* per_seq;
+    double* sums;  // a of every sequence, already divided for the mean
+    unsigned long long* pairs;
+};
+
+// First and last row of a sequence, within bounds whatever the offsets are.
+__device__ __forceinline__ void rows_of(const Rows& q, int seq, long long& lo, long long& hi) {
+    lo = load_int(q.offsets, seq, q.offset_bytes);
+    hi = load_int(q.offsets, seq + 1, q.offset_bytes);
+    lo = lo < 0 ? 0 : lo;
+    hi = hi > q.rows ? q.rows : hi;
+}
+
+// Sum (in 64 bits: sums of many thousand terms are subtracted from one another) and count of a sequence, by `n` threads of which this is `at`.
+__device__ __forceinline__ void sequence_sum(const PreferArgs& A, int seq, int at, int n, double& sum, int& count) {
+    long long lo, hi;
+    rows_of(A.q, seq, lo, hi);
+    sum = 0.0;
+    count = 0;
+    for (long long r = lo + at; r < hi; r += n) {
+        if (!row_counts(A.q, r)) continue;
+        sum += (double)A.logp[r] - (A.ref ? (double)A.ref[r] : 0.0);
+        ++count;
+    }
+}
+
+__device__ __forceinline__ double softplus(double v) { return (v > 0.0 ? v : 0.0) + log1p(exp(-fabs(v))); }
+
+// Loss of a pair and its derivative by z.
+__device__ __forceinline__ void pair_terms(const PreferArgs& A, double z, double& loss, double& dz) {
+    if (A.kind == ANAKIN_PREFER_SIGMOID) {
+        const double e = (double)A.smoothing;
+        loss = (1.0 - e) * softplus(-z) + e * softplus(z);
+        dz = 1.0 / (1.0 + exp(-z)) - (1.0 - e);
+    } else if (A.kind == ANAKIN_PREFER_HINGE) {
+        loss = z < 1.0 ? 1.0 - z : z >= 1.0 ? 0.0 : z;
+        dz = z >= 1.0 ? 0.0 : -1.0;
+        if (z != z) dz = z;
+    } else {
+        const double b = (double)A.beta, h = (z - 0.5) / b;
+        loss = h * h;
+        dz = 2.0 * h / b;
+    }
+}
+
+__global__ void __launch_bounds__(256) k_prefer_sums(PreferArgs A) {
+    PDL_START();
+    __shared__ double red[8];
+    for (int seq = blockIdx.x; seq < 2 * A.P; seq += gridDim.x) {
+        double sum;
+        int count;
+        sequence_sum(A, seq, threadIdx.x, 256, sum, count);
+        sum = block_sum(sum, red);
+        count = (int)block_sum((double)count, red);
+        if (threadIdx.x == 0) {
+            A.sums[seq] = A.mean && count > 0 ? sum / count : sum;
+            A.per_seq[seq] = count;
+        }
+    }
+}
+
+__device__ __forceinline__ bool pair_counts(const PreferArgs& A, const int* per_seq, int p) { return per_seq[p] > 0 && per_seq[A.P + p] > 0; }
+__device__ __forceinline__ double pair_z(const PreferArgs& A, const double* sums, int p) {
+    return (double)A.beta * (sums[p] - sums[A.P + p]) - (double)A.margin;
+}
+
+// Statistics and margins by one CTA.
+template <int THREADS>
+__device__ __forceinline__ void prefer_stats(const PreferArgs& A, const int* per_seq, const double* sums, double* red, unsigned long long* pairs_out) {
+    double v[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
+    for (int p = threadIdx.x; p < A.P; p += THREADS) {
+        const bool in = pair_counts(A, per_seq, p);
+        const double z = in ? pair_z(A, sums, p) : 0.0;
+        A.zout[p] = (float)z;
+        if (!in) continue;
+        double loss, dz;
+        pair_terms(A, z, loss, dz);
+        v[0] += loss;
+        v[1] += z > 0.0 ? 1.0 : 0.0;
+        v[2] += (double)A.beta * sums[p];
+        v[3] += (double)A.beta * sums[A.P + p];
+        v[4] += z;
+        v[5] += 1.0;
+    }
+#pragma unroll
+    for (int k = 0; k < 6; ++k) v[k] = block_sum(v[k], red);
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < ANAKIN_PREFERENCE_STATS; ++k) A.stats[k] = v[5] > 0.0 ? (float)(v[k] / v[5]) : 0.f;
+        *pairs_out = (unsigned long long)v[5];
+    }
+}
+
+__global__ void __launch_bounds__(1024) k_prefer_stats(PreferArgs A) {
+    PDL_START();
+    __shared__ double red[32];
+    prefer_stats<1024>(A, A.per_seq, A.sums, red, A.pairs);
+}
+
+__device__ __forceinline__ void prefer_row(const PreferArgs& A, long long r, const int* per_seq, const double* sums, unsigned long long pairs) {
+    float g = 0.f;
+    if (row_counts(A.q, r)) {
+        const int seq = sequence_of(A.q, r);
+        if (seq >= 0 && seq < 2 * A.P) {
+            const int p = seq < A.P ? seq : seq - A.P;
+            if (pair_counts(A, per_seq, p)) {
+                double loss, dz;
+                pair_terms(A, pair_z(A, sums, p), loss, dz);
+                double d = (double)A.beta * dz / (double)pairs;
+                if (A.mean) d /= per_seq[seq];
+                g = (float)(seq < A.P ? d : -d);
+            }
+        }
+    }
+    A.dlogp[r] = g;
+}
+
+__global__ void __launch_bounds__(256) k_prefer_rows(PreferArgs A) {
+    PDL_START();
+    const unsigned long long pairs = *A.pairs;
+    for (long long r = (long long)blockIdx.x * 256 + threadIdx.x; r < A.q.rows; r += (long long)gridDim.x * 256) prefer_row(A, r, A.per_seq, A.sums, pairs);
+}
+
+int grid_for(long long rows, int per_cta, int most) {
+    const long long n = (rows + per_cta - 1) / per_cta;
+    return (int)(n < 1 ? 1 : n < most ? n : most);
+}
+
+}  // namespace
+
+cudaError_t launch_counts(const Rows& q, Counts* c, int* per_seq, cudaStream_t s) {
+    cudaError_t e = cudaMemsetAsync(c, 0, sizeof(Counts), s);
+    if (e == cudaSuccess && per_seq && q.sequences > 0) e = cudaMemsetAsync(per_seq, 0, sizeof(int) * (size_t)q.sequences, s);
+    if (e != cudaSuccess) return e;
+    return launch<k_token_counts>(dim3(grid_for(q.rows, 256, 148 * 8)), dim3(256), 0, s, q, c, per_seq);
+}
+
+cudaError_t launch_policy_stats(const double* part, int n, const Objective& o, float* stats, cudaStream_t s) {
+    return launch<k_policy_stats>(dim3(1), dim3(256), 0, s, part, n, o, stats);
+}
+
+}  // namespace tok
+}  // namespace anakin
+
+using namespace anakin;
+using namespace anakin::tok;
+
+extern "C" {
+
+int anakin_token_workspace_bytes(int64_t rows, int64_t sequences, size_t* bytes) {
+    if (!bytes || rows < 0 || sequences < 0 || rows >= (int64_t(1) << 31) || sequences >= (int64_t(1) << 31) - 1) return ANAKIN_E_INVALID_ARG;
+    *bytes = carve(nullptr, sequences < 1 ? 1 : sequences).bytes;
+    return ANAKIN_OK;
+}
+
+int anakin_token_policy_loss(const anakin_token_rows* rows, const anakin_policy_objective* objective, const float* logp, const float* old_logp,
+                             const float* adv, const float* ref_logp, const float* entropy, float* stats, float* dlogp, float* dentropy,
+                             void* dev_workspace, size_t bytes, void* cuda_stream) {
+    PolicyArgs2 A = {};
+    int rc = check_rows(rows, false, false, false, &A.q);
+    if (rc == ANAKIN_OK) rc = check_policy(objective, &A.o);
+    if (rc != ANAKIN_OK) return rc;
+    const bool empty = A.q.rows == 0;
+    if (!stats || (!empty && (!logp || !adv || !dlogp || (A.o.kl != ANAKIN_KL_NONE && !ref_logp)))) return ANAKIN_E_INVALID_ARG;
+    if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
+    const Workspace w = carve(dev_workspace, A.q.sequences);
+    if (bytes < w.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    A.logp = logp;
+    A.old_logp = old_logp;
+    A.adv = adv;
+    A.ref = A.o.kl != ANAKIN_KL_NONE ? ref_logp : nullptr;
+    A.entropy = entropy;
+    A.stats = stats;
+    A.dlogp = dlogp;
+    A.dentropy = dentropy;
+    A.counts = w.counts;
+    A.per_seq = w.per_seq;
+    A.part = w.part;
+    if (A.q.rows <= kSmallRows && A.q.sequences <= kSmallSeqs) {
+        return launch<k_policy_loss_small>(dim3(1), dim3(1024), 0, s, A) == cudaSuccess ? ANAKIN_OK : fail();
+    }
+    if (A.o.mean != ANAKIN_MEAN_FIXED && launch_counts(A.q, w.counts, A.o.mean == ANAKIN_MEAN_SEQUENCE ? w.per_seq : nullptr, s) != cudaSuccess) return fail();
+    const int grid = grid_for(A.q.rows, 256, kMaxPartials);
+    if (launch<k_policy_loss>(dim3(grid), dim3(256), 0, s, A) != cudaSuccess) return fail();
+    return launch_policy_stats(w.part, grid, A.o, stats, s) == cudaSuccess ? ANAKIN_OK : fail();
+}
+
+int anakin_token_preference_loss(const anakin_token_rows* rows, const anakin_preference_objective* objective, const float* logp,
+                                 const float* ref_logp, float* stats, float* margin, float* dlogp, void* dev_workspace, size_t bytes,
+                                 void* cuda_stream) {
+    PreferArgs A = {};
+    const int rc = check_rows(rows, false, false, true, &A.q);
+    if (rc != ANAKIN_OK) return rc;
+    const anakin_preference_objective* p = objective;
+    if (!p || p->struct_size != sizeof(*p) || p->kind < ANAKIN_PREFER_SIGMOID || p->kind > ANAKIN_PREFER_SQUARED || !(p->beta > 0.f) ||
+        !(p->beta < INFINITY) || p->margin != p->margin || !(p->smoothing >= 0.f && p->smoothing <= 0.5f) || (p->mean != 0 && p->mean != 1))
+        return ANAKIN_E_INVALID_ARG;
+    if (A.q.sequences % 2 != 0 || !stats || (A.q.sequences > 0 && !margin) || (A.q.rows > 0 && (!logp || !dlogp))) return ANAKIN_E_INVALID_ARG;
+    if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
+    const Workspace w = carve(dev_workspace, A.q.sequences);
+    if (bytes < w.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    A.P = A.q.sequences / 2;
+    A.kind = p->kind;
+    A.mean = p->mean;
+    A.beta = p->beta;
+    A.margin = p->margin;
+    A.smoothing = p->smoothing;
+    A.logp = logp;
+    A.ref = ref_logp;
+    A.stats = stats;
+    A.zout = margin;
+    A.dlogp = dlogp;
+    A.per_seq = w.per_seq;
+    A.sums = w.sums;
+    A.pairs = &w.counts->rows;
+    if (A.P > 0 && launch<k_prefer_sums>(dim3(grid_for(2 * A.P, 1, 148 * 16)), dim3(256), 0, s, A) != cudaSuccess) return fail();
+    if (launch<k_prefer_stats>(dim3(1), dim3(1024), 0, s, A) != cudaSuccess) return fail();
+    if (A.q.rows > 0 && launch<k_prefer_rows>(dim3(grid_for(A.q.rows, 256, 148 * 8)), dim3(256), 0, s, A) != cudaSuccess) return fail();
+    return ANAKIN_OK;
+}
+
+}  // extern "C"
