@@ -351,22 +351,30 @@ __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.lau
 // SMs with room, and run there side by side while others stay empty (k_vtrace behind the H = 64 rollout: 37 -> 61 us).
 #define PDL_START() do { anakin::pdl_wait(); anakin::pdl_trigger(); } while (0)
 
-// Launches kernel K.  Its limit of dynamic shared memory is raised to all there is, once per device instead of before every launch.
+// Raises kernel K's limit of dynamic shared memory to all there is, once per device instead of before every launch.
+template <auto K>
+inline cudaError_t allow_shared() {
+    constexpr int MAXDEV = 64;
+    static std::atomic<bool> raised[MAXDEV];  // (zero-initialised)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= MAXDEV || !raised[dev].load(std::memory_order_acquire)) {
+        cudaFuncAttributes fa;
+        e = cudaFuncGetAttributes(&fa, K);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
+        if (e != cudaSuccess) return e;
+        if (dev < MAXDEV) raised[dev].store(true, std::memory_order_release);
+    }
+    return cudaSuccess;
+}
+
+// Launches kernel K.
 template <auto K, class... A>
 inline cudaError_t launch(dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
     if (smem > 48 * 1024) {
-        constexpr int MAXDEV = 64;
-        static std::atomic<bool> raised[MAXDEV];  // (zero-initialised)
-        int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
+        const cudaError_t e = allow_shared<K>();
         if (e != cudaSuccess) return e;
-        if (dev >= MAXDEV || !raised[dev].load(std::memory_order_acquire)) {
-            cudaFuncAttributes fa;
-            e = cudaFuncGetAttributes(&fa, K);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
-            if (e != cudaSuccess) return e;
-            if (dev < MAXDEV) raised[dev].store(true, std::memory_order_release);
-        }
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -378,6 +386,29 @@ inline cudaError_t launch(dim3 grid, dim3 block, size_t smem, cudaStream_t s, A.
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, K, args...);
+}
+
+// The same in clusters of C blocks.
+template <auto K, class... A>
+inline cudaError_t launch_cluster(dim3 grid, dim3 block, size_t smem, cudaStream_t s, int C, A... args) {
+    if (smem > 48 * 1024) {
+        const cudaError_t e = allow_shared<K>();
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = C;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, K, args...);
 }
 #endif

@@ -51,7 +51,7 @@ int check_policy(const anakin_policy_objective* p, Objective* o) {
     return ANAKIN_OK;
 }
 
-Workspace carve(void* base, long long sequences) {
+Workspace carve(void* base, long long rows, long long sequences) {
     size_t off = 0;
     auto take = [&](size_t bytes) { void* p = static_cast<unsigned char*>(base) + off; off += (bytes + 255) / 256 * 256; return p; };
     Workspace w;
@@ -59,6 +59,7 @@ Workspace carve(void* base, long long sequences) {
     w.part = static_cast<double*>(take(sizeof(double) * kMaxPartials * kPolicyParts));
     w.per_seq = static_cast<int*>(take(sizeof(int) * (size_t)sequences));
     w.sums = static_cast<double*>(take(sizeof(double) * (size_t)sequences));
+    w.info = static_cast<int*>(take(sizeof(int) * (size_t)rows));
     w.bytes = off;
     return w;
 }
@@ -78,8 +79,8 @@ __device__ __forceinline__ void add_counts(bool counts, int seq, unsigned long l
     if (lane == __ffs(same) - 1 && atomicAdd(&per_seq[seq], __popc(same)) == 0) atomicAdd(seqs, 1ull);
 }
 
-__global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* per_seq) {
-    PDL_START();
+__global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* per_seq, int* info) {
+    pdl_wait();  // (no early trigger: blocks of the next kernel placed around this one's would leave its clusters without room, a wave late)
     const long long stride = (long long)gridDim.x * 256;
     for (long long r0 = (long long)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < q.rows; r0 += stride) {
         const long long r = r0 + (threadIdx.x & 31);
@@ -88,8 +89,12 @@ __global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* pe
         if (counts) {
             seq = sequence_of(q, r);
             counts = seq >= 0 && seq < q.sequences;
+            if (!counts) seq = -1;
+        } else {
+            seq = -2;
         }
-        add_counts(counts, seq, &c->rows, &c->sequences, per_seq);
+        if (info && r < q.rows) info[r] = seq;
+        if (c) add_counts(counts, seq, &c->rows, &c->sequences, per_seq);
     }
 }
 
@@ -327,11 +332,14 @@ int grid_for(long long rows, int per_cta, int most) {
 
 }  // namespace
 
-cudaError_t launch_counts(const Rows& q, Counts* c, int* per_seq, cudaStream_t s) {
-    cudaError_t e = cudaMemsetAsync(c, 0, sizeof(Counts), s);
-    if (e == cudaSuccess && per_seq && q.sequences > 0) e = cudaMemsetAsync(per_seq, 0, sizeof(int) * (size_t)q.sequences, s);
+cudaError_t launch_counts(const Rows& q, int mean, const Workspace& w, cudaStream_t s) {
+    const bool by_seq = mean == ANAKIN_MEAN_SEQUENCE;
+    cudaError_t e = cudaSuccess;
+    if (mean != ANAKIN_MEAN_FIXED) e = cudaMemsetAsync(w.counts, 0, sizeof(Counts), s);
+    if (e == cudaSuccess && by_seq && q.sequences > 0) e = cudaMemsetAsync(w.per_seq, 0, sizeof(int) * (size_t)q.sequences, s);
     if (e != cudaSuccess) return e;
-    return launch<k_token_counts>(dim3(grid_for(q.rows, 256, 148 * 8)), dim3(256), 0, s, q, c, per_seq);
+    return launch<k_token_counts>(dim3(grid_for(q.rows, 256, 148 * 8)), dim3(256), 0, s, q, mean != ANAKIN_MEAN_FIXED ? w.counts : nullptr,
+                                  by_seq ? w.per_seq : nullptr, w.info);
 }
 
 cudaError_t launch_policy_stats(const double* part, int n, const Objective& o, float* stats, cudaStream_t s) {
@@ -348,7 +356,7 @@ extern "C" {
 
 int anakin_token_workspace_bytes(int64_t rows, int64_t sequences, size_t* bytes) {
     if (!bytes || rows < 0 || sequences < 0 || rows >= (int64_t(1) << 31) || sequences >= (int64_t(1) << 31) - 1) return ANAKIN_E_INVALID_ARG;
-    *bytes = carve(nullptr, sequences < 1 ? 1 : sequences).bytes;
+    *bytes = carve(nullptr, rows, sequences < 1 ? 1 : sequences).bytes;
     return ANAKIN_OK;
 }
 
@@ -362,7 +370,7 @@ int anakin_token_policy_loss(const anakin_token_rows* rows, const anakin_policy_
     const bool empty = A.q.rows == 0;
     if (!stats || (!empty && (!logp || !adv || !dlogp || (A.o.kl != ANAKIN_KL_NONE && !ref_logp)))) return ANAKIN_E_INVALID_ARG;
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
-    const Workspace w = carve(dev_workspace, A.q.sequences);
+    const Workspace w = carve(dev_workspace, A.q.rows, A.q.sequences);
     if (bytes < w.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     A.logp = logp;
@@ -379,7 +387,7 @@ int anakin_token_policy_loss(const anakin_token_rows* rows, const anakin_policy_
     if (A.q.rows <= kSmallRows && A.q.sequences <= kSmallSeqs) {
         return launch<k_policy_loss_small>(dim3(1), dim3(1024), 0, s, A) == cudaSuccess ? ANAKIN_OK : fail();
     }
-    if (A.o.mean != ANAKIN_MEAN_FIXED && launch_counts(A.q, w.counts, A.o.mean == ANAKIN_MEAN_SEQUENCE ? w.per_seq : nullptr, s) != cudaSuccess) return fail();
+    if (A.o.mean != ANAKIN_MEAN_FIXED && launch_counts(A.q, A.o.mean, w, s) != cudaSuccess) return fail();
     const int grid = grid_for(A.q.rows, 256, kMaxPartials);
     if (launch<k_policy_loss>(dim3(grid), dim3(256), 0, s, A) != cudaSuccess) return fail();
     return launch_policy_stats(w.part, grid, A.o, stats, s) == cudaSuccess ? ANAKIN_OK : fail();
@@ -397,7 +405,7 @@ int anakin_token_preference_loss(const anakin_token_rows* rows, const anakin_pre
         return ANAKIN_E_INVALID_ARG;
     if (A.q.sequences % 2 != 0 || !stats || (A.q.sequences > 0 && !margin) || (A.q.rows > 0 && (!logp || !dlogp))) return ANAKIN_E_INVALID_ARG;
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
-    const Workspace w = carve(dev_workspace, A.q.sequences);
+    const Workspace w = carve(dev_workspace, A.q.rows, A.q.sequences);
     if (bytes < w.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     A.P = A.q.sequences / 2;

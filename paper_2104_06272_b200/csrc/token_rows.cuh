@@ -163,8 +163,6 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 
 // Rows of partial statistics, one for each CTA of a kernel, summed in order by one CTA (see token_loss.cu).
 cudaError_t launch_policy_stats(const double* part, int n, const Objective& o, float* stats, cudaStream_t s);
-// Counts of the rows (and, with per_seq, of each sequence) into the workspace.
-cudaError_t launch_counts(const Rows& q, Counts* c, int* per_seq, cudaStream_t s);
 
 constexpr int kPolicyParts = 5;         // sums a CTA leaves: pg, kl, H, cut, old - l
 constexpr int kMaxPartials = 148 * 16;  // CTAs that may leave some
@@ -175,9 +173,13 @@ struct Workspace {
     double* part;   // [kMaxPartials][kPolicyParts]
     int* per_seq;   // [sequences]
     double* sums;   // [sequences] of the preference loss
+    int* info;      // [rows] of the policy gradient: the row's sequence; -1: no part in the loss, -2: does not count at all
     size_t bytes;
 };
-Workspace carve(void* base, long long sequences);
+Workspace carve(void* base, long long rows, long long sequences);
+
+// What the means divide by (ANAKIN_MEAN_*), and every row's sequence, into the workspace.
+cudaError_t launch_counts(const Rows& q, int mean, const Workspace& w, cudaStream_t s);
 
 // Host: checks of what every call has in common; fills q.
 int check_rows(const anakin_token_rows* rows, bool need_logits, bool need_tokens, bool need_offsets, Rows* q);

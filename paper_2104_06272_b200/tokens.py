@@ -9,6 +9,7 @@ refuses with AnakinError before anything is enqueued.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import NamedTuple
 
 import torch
@@ -112,42 +113,46 @@ def _ck(rc: int):
         raise AnakinError(rc)
 
 
-def _ptr(t: torch.Tensor | None):
-    return None if t is None else _vp(t.data_ptr())
+_F32 = torch.float32
+_TOKEN_ROWS = C.sizeof(TokenRows)
+_stream_of = torch._C._cuda_getCurrentRawStream  # the device's current stream as an integer
 
 
-def _on(dev: torch.device, name: str, t, dtype, shape) -> torch.Tensor | None:
-    """t, a dense tensor of that device, type and shape, or None."""
+def _vector(name: str, t, n: int, dev: torch.device, dtypes=(_F32,)) -> int | None:
+    """Address of t, a dense vector of n numbers on that device; None stays None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.device != dev or tuple(t.shape) != tuple(shape) or t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
-        _refuse(f"{name}: a tensor of {dtype}, shape {tuple(shape)}, on {dev} is needed")
-    return t if t.is_contiguous() else _refuse(f"{name} is not contiguous")
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != 1 or t.shape[0] != n or t.device != dev or not t.is_contiguous():
+        _refuse(f"{name}: a dense vector of {n} numbers ({', '.join(map(str, dtypes))}) on {dev} is needed")
+    return t.data_ptr()
 
 
 def _matrix(name: str, t, dev=None, dtype=None, shape=None) -> tuple[int, int, int]:
     """(rows, cols, elements from row to row) of a matrix whose rows are dense."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype not in DTYPES or t.shape[1] < 1:
         _refuse(f"{name}: a CUDA matrix of float32, bfloat16 or float16 with at least one column is needed")
-    if (dev is not None and t.device != dev) or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)):
-        _refuse(f"{name}: {dtype} of shape {tuple(shape)} on {dev} is needed")
     rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+    if (dev is not None and t.device != dev) or (dtype is not None and t.dtype is not dtype) or (shape is not None and (rows, cols) != shape):
+        _refuse(f"{name}: {dtype or 'a matrix'} of shape {shape} on {dev} is needed")
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         _refuse(f"{name}: columns have to lie side by side, and rows one after the other")
-    return rows, cols, (t.stride(0) if rows > 1 else cols)
+    return rows, cols, ld if rows > 1 else cols
 
 
 class _Device:
     """Makes the tensors' device current for the call and gives its current stream."""
 
-    def __init__(self, dev: torch.device):
-        self.dev = dev
-        self.guard = torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else None
+    __slots__ = ("index", "guard")
 
-    def __enter__(self):
-        if self.guard is not None:
+    def __init__(self, dev: torch.device):
+        self.index, self.guard = dev.index, None
+
+    def __enter__(self) -> int:
+        if self.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.index)
             self.guard.__enter__()
-        return _vp(torch.cuda.current_stream(self.dev).cuda_stream)
+        return _stream_of(self.index)
 
     def __exit__(self, *exc):
         if self.guard is not None:
@@ -157,66 +162,74 @@ class _Device:
 _INTS, _FLAGS = (torch.int64, torch.int32), (torch.bool, torch.uint8)
 
 
-def _token_rows(dev, rows, tokens, mask=None, offsets=None, logits=None, scale=1.0) -> TokenRows:
-    r = TokenRows(struct_size=C.sizeof(TokenRows), rows=rows, scale=scale)
+def _token_rows(dev, n, tokens, mask, offsets, logits=None, vocab=0, ld=0, scale=1.0) -> TokenRows:
+    r = TokenRows(_TOKEN_ROWS, 0, n, vocab, ld)
+    r.scale = scale
     if logits is not None:
-        _, r.vocab, r.ld = _matrix("logits", logits)
         r.dtype, r.logits = DTYPES[logits.dtype], logits.data_ptr()
-    if _on(dev, "tokens", tokens, _INTS, (rows,)) is not None:
-        r.tokens, r.token_bytes = tokens.data_ptr(), tokens.element_size()
-    if _on(dev, "mask", mask, _FLAGS, (rows,)) is not None:
-        r.mask = mask.data_ptr()
+    if tokens is not None:
+        r.tokens, r.token_bytes = _vector("tokens", tokens, n, dev, _INTS), tokens.element_size()
+    if mask is not None:
+        r.mask = _vector("mask", mask, n, dev, _FLAGS)
     if offsets is not None:
-        if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 1:
+        count = offsets.numel() if isinstance(offsets, torch.Tensor) else 0
+        if count < 1:
             _refuse("offsets: one number more than there are sequences")
-        _on(dev, "offsets", offsets, _INTS, tuple(offsets.shape))
-        r.offsets, r.offset_bytes, r.sequences = offsets.data_ptr(), offsets.element_size(), offsets.numel() - 1
+        r.offsets, r.offset_bytes, r.sequences = _vector("offsets", offsets, count, dev, _INTS), offsets.element_size(), count - 1
     return r
 
 
-def _workspace(dev, rows: TokenRows) -> torch.Tensor:
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(rows: int, sequences: int) -> int:
     n = C.c_size_t(0)
-    _ck(_lib.anakin_token_workspace_bytes(rows.rows, rows.sequences, C.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=dev)
+    _ck(_lib.anakin_token_workspace_bytes(rows, sequences, C.byref(n)))
+    return n.value
 
 
-def _like(name: str, out, like: torch.Tensor, shape=None) -> torch.Tensor:
+def _floats(dev, *sizes: int) -> list[torch.Tensor]:
+    """Vectors of these lengths, one allocation (an allocation costs more than the smallest kernels)."""
+    return list(torch.empty(sum(sizes), device=dev).split(sizes))
+
+
+def _like(name: str, out, like: torch.Tensor) -> tuple[torch.Tensor, int]:
+    """A matrix like `like`, and its elements from row to row."""
+    rows, cols = like.shape
     if out is None:
-        return torch.empty(shape or tuple(like.shape), dtype=like.dtype, device=like.device)
-    _matrix(name, out, like.device, like.dtype, shape or tuple(like.shape))
-    return out
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+        return torch.empty((rows, cols), dtype=like.dtype, device=like.device), cols
+    return out, _matrix(name, out, like.device, like.dtype, (rows, cols))[2]
 
 
 def logp(logits: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, mask: torch.Tensor | None = None, entropy: bool = True) -> TokenLogp:
     """Log-probability of every row's token under softmax(scale * logits), and the entropy (anakin_token_logp)."""
-    n, _, _ = _matrix("logits", logits)
+    n, vocab, ld = _matrix("logits", logits)
     dev = logits.device
     if tokens is None:
         _refuse("tokens are needed")
     with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, None, logits, scale)
-        out = TokenLogp(torch.empty(n, device=dev), torch.empty(n, device=dev) if entropy else None, torch.empty(n, 2, device=dev))
-        _ck(_lib.anakin_token_logp(C.byref(rows), _ptr(out.logp), _ptr(out.entropy), _ptr(out.norm), stream))
-    return out
+        rows = _token_rows(dev, n, tokens, mask, None, logits, vocab, ld, scale)
+        if entropy:
+            norm, lp, ent = _floats(dev, 2 * n, n, n)
+        else:
+            (norm, lp), ent = _floats(dev, 2 * n, n), None
+        _ck(_lib.anakin_token_logp(rows, lp.data_ptr(), ent.data_ptr() if entropy else None, norm.data_ptr(), stream))
+    return TokenLogp(lp, ent, norm.view(n, 2))
 
 
 def logp_backward(logits: torch.Tensor, tokens: torch.Tensor, norm: torch.Tensor, dlogp: torch.Tensor, entropy: torch.Tensor | None = None,
                   dentropy: torch.Tensor | None = None, scale: float = 1.0, mask: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient of the logits from those of logp and entropy (anakin_token_logp_backward).  norm and entropy come from logp() with the same
     tokens, scale and mask; `out` may be the logits themselves."""
-    n, _, _ = _matrix("logits", logits)
-    dev, f32 = logits.device, torch.float32
-    if tokens is None or norm is None or dlogp is None or (dentropy is not None and entropy is None):
+    n, vocab, ld = _matrix("logits", logits)
+    dev = logits.device
+    if tokens is None or dlogp is None or (dentropy is not None and entropy is None):
         _refuse("tokens, norm and dlogp are needed, and entropy with dentropy")
+    if _matrix("norm", norm, dev, _F32, (n, 2))[2] != 2:
+        _refuse("norm: its rows lie one behind the other")
     with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, None, logits, scale)
-        _on(dev, "norm", norm, f32, (n, 2)), _on(dev, "dlogp", dlogp, f32, (n,)), _on(dev, "entropy", entropy, f32, (n,)), _on(dev, "dentropy", dentropy, f32, (n,))
-        out = _like("out", out, logits)
-        _ck(_lib.anakin_token_logp_backward(C.byref(rows), _ptr(norm), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(out), _ld(out), stream))
+        rows = _token_rows(dev, n, tokens, mask, None, logits, vocab, ld, scale)
+        out, ld_out = _like("out", out, logits)
+        _ck(_lib.anakin_token_logp_backward(rows, norm.data_ptr(), _vector("entropy", entropy, n, dev), _vector("dlogp", dlogp, n, dev),
+                                            _vector("dentropy", dentropy, n, dev), out.data_ptr(), ld_out, stream))
     return out
 
 
@@ -226,37 +239,41 @@ def policy_loss(objective: PolicyObjective, logp: torch.Tensor, old_logp: torch.
     """The clipped policy loss from log-probabilities, and its gradients (anakin_token_policy_loss)."""
     if not isinstance(logp, torch.Tensor) or not logp.is_cuda or logp.dim() != 1:
         _refuse("logp: a CUDA vector is needed")
-    n, dev, f32 = logp.numel(), logp.device, torch.float32
-    for name, t in (("logp", logp), ("old_logp", old_logp), ("adv", adv), ("ref_logp", ref_logp), ("entropy", entropy)):
-        _on(dev, name, t, f32, (n,))
     if adv is None or (objective.kl != 0 and ref_logp is None):
         _refuse("adv is needed, and ref_logp with a KL term")
+    n, dev = logp.shape[0], logp.device
     with _Device(dev) as stream:
         rows = _token_rows(dev, n, tokens, mask, offsets)
-        ws = _workspace(dev, rows)
-        out = PolicyLoss(torch.empty(len(POLICY_STATS), device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev) if entropy is not None else None)
-        _ck(_lib.anakin_token_policy_loss(C.byref(rows), C.byref(objective), _ptr(logp), _ptr(old_logp), _ptr(adv), _ptr(ref_logp), _ptr(entropy),
-                                          _ptr(out.stats), _ptr(out.dlogp), _ptr(out.dentropy), _ptr(ws), ws.numel(), stream))
-    return out
+        size = _workspace_bytes(n, rows.sequences)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        if entropy is not None:
+            stats, dlogp, dentropy = _floats(dev, len(POLICY_STATS), n, n)
+        else:
+            (stats, dlogp), dentropy = _floats(dev, len(POLICY_STATS), n), None
+        _ck(_lib.anakin_token_policy_loss(rows, objective, _vector("logp", logp, n, dev), _vector("old_logp", old_logp, n, dev), _vector("adv", adv, n, dev),
+                                          _vector("ref_logp", ref_logp, n, dev), _vector("entropy", entropy, n, dev), stats.data_ptr(), dlogp.data_ptr(),
+                                          None if dentropy is None else dentropy.data_ptr(), ws.data_ptr(), size, stream))
+    return PolicyLoss(stats, dlogp, dentropy)
 
 
 def policy_grad(objective: PolicyObjective, logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor | None, adv: torch.Tensor,
                 ref_logp: torch.Tensor | None = None, mask: torch.Tensor | None = None, offsets: torch.Tensor | None = None, scale: float = 1.0,
                 out: torch.Tensor | None = None) -> PolicyGrad:
     """The clipped policy loss from logits, with the gradient of the logits (anakin_token_policy_grad); `out` may be the logits themselves."""
-    n, _, _ = _matrix("logits", logits)
-    dev, f32 = logits.device, torch.float32
-    for name, t in (("old_logp", old_logp), ("adv", adv), ("ref_logp", ref_logp)):
-        _on(dev, name, t, f32, (n,))
+    n, vocab, ld = _matrix("logits", logits)
+    dev = logits.device
     if tokens is None or adv is None or (objective.kl != 0 and ref_logp is None):
         _refuse("tokens and adv are needed, and ref_logp with a KL term")
     with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, offsets, logits, scale)
-        ws = _workspace(dev, rows)
-        o = PolicyGrad(torch.empty(len(POLICY_STATS), device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev), _like("out", out, logits))
-        _ck(_lib.anakin_token_policy_grad(C.byref(rows), C.byref(objective), _ptr(old_logp), _ptr(adv), _ptr(ref_logp), _ptr(o.stats), _ptr(o.logp),
-                                          _ptr(o.entropy), _ptr(o.dlogits), _ld(o.dlogits), _ptr(ws), ws.numel(), stream))
-    return o
+        rows = _token_rows(dev, n, tokens, mask, offsets, logits, vocab, ld, scale)
+        size = _workspace_bytes(n, rows.sequences)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        stats, lp, ent = _floats(dev, len(POLICY_STATS), n, n)
+        out, ld_out = _like("out", out, logits)
+        _ck(_lib.anakin_token_policy_grad(rows, objective, _vector("old_logp", old_logp, n, dev), _vector("adv", adv, n, dev),
+                                          _vector("ref_logp", ref_logp, n, dev), stats.data_ptr(), lp.data_ptr(), ent.data_ptr(), out.data_ptr(), ld_out,
+                                          ws.data_ptr(), size, stream))
+    return PolicyGrad(stats, lp, ent, out)
 
 
 def preference_loss(objective: PreferenceObjective, logp: torch.Tensor, offsets: torch.Tensor, ref_logp: torch.Tensor | None = None,
@@ -264,26 +281,29 @@ def preference_loss(objective: PreferenceObjective, logp: torch.Tensor, offsets:
     """The preference loss over pairs of sequences, the preferred ones first, and its gradient (anakin_token_preference_loss)."""
     if not isinstance(logp, torch.Tensor) or not logp.is_cuda or logp.dim() != 1:
         _refuse("logp: a CUDA vector is needed")
-    n, dev = logp.numel(), logp.device
-    _on(dev, "logp", logp, torch.float32, (n,)), _on(dev, "ref_logp", ref_logp, torch.float32, (n,))
-    if offsets is None or not isinstance(offsets, torch.Tensor) or offsets.numel() % 2 == 0:
+    if not isinstance(offsets, torch.Tensor) or offsets.numel() % 2 == 0:
         _refuse("offsets of an even number of sequences are needed")
+    n, dev = logp.shape[0], logp.device
     with _Device(dev) as stream:
         rows = _token_rows(dev, n, tokens, mask, offsets)
-        ws = _workspace(dev, rows)
-        out = PreferenceLoss(torch.empty(len(PREFERENCE_STATS), device=dev), torch.empty(rows.sequences // 2, device=dev), torch.empty(n, device=dev))
-        _ck(_lib.anakin_token_preference_loss(C.byref(rows), C.byref(objective), _ptr(logp), _ptr(ref_logp), _ptr(out.stats), _ptr(out.margin),
-                                              _ptr(out.dlogp), _ptr(ws), ws.numel(), stream))
-    return out
+        size = _workspace_bytes(n, rows.sequences)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        stats, margin, dlogp = _floats(dev, len(PREFERENCE_STATS), rows.sequences // 2, n)
+        _ck(_lib.anakin_token_preference_loss(rows, objective, _vector("logp", logp, n, dev), _vector("ref_logp", ref_logp, n, dev), stats.data_ptr(),
+                                              margin.data_ptr(), dlogp.data_ptr(), ws.data_ptr(), size, stream))
+    return PreferenceLoss(stats, margin, dlogp)
 
 
 def _checkpoint(ck: Checkpoint) -> tuple[torch.device, int, int]:
-    blocks = (ck.cols + 31) // 32
-    if ck.cols < 1 or not isinstance(ck.codes, torch.Tensor) or not ck.codes.is_cuda or ck.codes.dim() != 2:
-        _refuse("codes: a CUDA matrix of uint8 is needed")
-    dev, rows = ck.codes.device, ck.codes.shape[0]
-    _on(dev, "codes", ck.codes, torch.uint8, (rows, blocks * 32)), _on(dev, "scales", ck.scales, torch.uint8, (rows, blocks))
-    return dev, rows, ck.cols
+    codes, scales, cols = ck
+    blocks = (cols + 31) // 32
+    if cols < 1 or not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dtype is not torch.uint8 or codes.dim() != 2 or codes.shape[1] != blocks * 32 or \
+            not codes.is_contiguous():
+        _refuse(f"codes: a dense CUDA matrix of uint8 with {blocks * 32} columns is needed")
+    rows = codes.shape[0]
+    if not isinstance(scales, torch.Tensor) or scales.dtype is not torch.uint8 or scales.shape != (rows, blocks) or scales.device != codes.device or not scales.is_contiguous():
+        _refuse(f"scales: a dense matrix of uint8, {rows} x {blocks}, is needed beside the codes")
+    return codes.device, rows, cols
 
 
 def ckpt_forward(x: torch.Tensor, act: str = "relu", y: bool = True, out: torch.Tensor | None = None) -> tuple[torch.Tensor | None, Checkpoint]:
@@ -291,35 +311,42 @@ def ckpt_forward(x: torch.Tensor, act: str = "relu", y: bool = True, out: torch.
     rows, cols, ld = _matrix("x", x)
     a, dev, blocks = _one_of(ACTS, "act", act), x.device, (cols + 31) // 32
     with _Device(dev) as stream:
-        res = _like("out", out, x) if y else None
-        ck = Checkpoint(torch.empty(rows, blocks * 32, dtype=torch.uint8, device=dev), torch.empty(rows, blocks, dtype=torch.uint8, device=dev), cols)
-        _ck(_lib.anakin_ckpt_forward(DTYPES[x.dtype], a, rows, cols, _ptr(x), ld, _ptr(res), _ld(res) if y else 0, _ptr(ck.codes), _ptr(ck.scales), stream))
-    return res, ck
+        res, ldy = _like("out", out, x) if y else (None, 0)
+        codes = torch.empty((rows, blocks * 32), dtype=torch.uint8, device=dev)
+        scales = torch.empty((rows, blocks), dtype=torch.uint8, device=dev)
+        _ck(_lib.anakin_ckpt_forward(DTYPES[x.dtype], a, rows, cols, x.data_ptr(), ld, res.data_ptr() if y else None, ldy, codes.data_ptr(), scales.data_ptr(), stream))
+    return res, Checkpoint(codes, scales, cols)
 
 
 def ckpt_unpack(ck: Checkpoint, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values that a checkpoint holds (anakin_ckpt_unpack)."""
     dev, rows, cols = _checkpoint(ck)
     if out is not None:
-        _matrix("out", out, dev, out.dtype, (rows, cols))
-        dtype = out.dtype
-    if dtype not in DTYPES:
+        ld, dtype = _matrix("out", out, dev, None, (rows, cols))[2], out.dtype
+    elif dtype not in DTYPES:
         _refuse("float32, bfloat16 or float16")
     with _Device(dev) as stream:
-        out = torch.empty(rows, cols, dtype=dtype, device=dev) if out is None else out
-        _ck(_lib.anakin_ckpt_unpack(DTYPES[dtype], rows, cols, _ptr(ck.codes), _ptr(ck.scales), _ptr(out), _ld(out), stream))
+        if out is None:
+            out, ld = torch.empty((rows, cols), dtype=dtype, device=dev), cols
+        _ck(_lib.anakin_ckpt_unpack(DTYPES[dtype], rows, cols, ck.codes.data_ptr(), ck.scales.data_ptr(), out.data_ptr(), ld, stream))
     return out
 
 
 def ckpt_backward(ck: Checkpoint, dy: torch.Tensor, act: str = "relu", out: torch.Tensor | None = None) -> torch.Tensor:
     """dy * act'(x) with x from its checkpoint (anakin_ckpt_backward); `out` may be dy itself."""
     dev, rows, cols = _checkpoint(ck)
-    _, _, ld = _matrix("dy", dy, dev, dy.dtype if isinstance(dy, torch.Tensor) else None, (rows, cols))
-    a = _one_of(ACTS, "act", act)
+    ld, a = _matrix("dy", dy, dev, None, (rows, cols))[2], _one_of(ACTS, "act", act)
     with _Device(dev) as stream:
-        out = _like("out", out, dy)
-        _ck(_lib.anakin_ckpt_backward(DTYPES[dy.dtype], a, rows, cols, _ptr(ck.codes), _ptr(ck.scales), _ptr(dy), ld, _ptr(out), _ld(out), stream))
+        out, ldx = _like("out", out, dy)
+        _ck(_lib.anakin_ckpt_backward(DTYPES[dy.dtype], a, rows, cols, ck.codes.data_ptr(), ck.scales.data_ptr(), dy.data_ptr(), ld, out.data_ptr(), ldx, stream))
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def _weight_grad_bytes(dtype: int, rows: int, cols: int, n: int) -> int:
+    size = C.c_size_t(0)
+    _ck(_lib.anakin_ckpt_weight_grad_workspace_bytes(dtype, rows, cols, n, C.byref(size)))
+    return size.value
 
 
 def ckpt_weight_grad(ck: Checkpoint, dy: torch.Tensor, act: str = "identity", out: torch.Tensor | None = None, accumulate: bool = False,
@@ -327,21 +354,21 @@ def ckpt_weight_grad(ck: Checkpoint, dy: torch.Tensor, act: str = "identity", ou
     """act(x)^T dy, f32 [cols][n], with x from its checkpoint (anakin_ckpt_weight_grad); accumulate adds to `out`.  `status` (int32 [1], zeroed by
     the caller) takes the device status bits."""
     dev, rows, cols = _checkpoint(ck)
-    r, n, ld = _matrix("dy", dy, dev, dy.dtype if isinstance(dy, torch.Tensor) else None, (rows, dy.shape[1]) if isinstance(dy, torch.Tensor) and dy.dim() == 2 else (rows, 1))
-    a = _one_of(ACTS, "act", act)
+    r, n, ld = _matrix("dy", dy, dev)
+    a, dt = _one_of(ACTS, "act", act), DTYPES[dy.dtype]
+    if r != rows:
+        _refuse(f"dy: {rows} rows are needed")
     if a > 1:
         _refuse("act is identity or relu here: checkpoint the activation's output", E_UNSUPPORTED_CFG)
-    if accumulate and out is None:
+    if out is not None:
+        ldw = _matrix("out", out, dev, _F32, (cols, n))[2]
+    elif accumulate:
         _refuse("accumulate adds to `out`")
-    _on(dev, "status", status, torch.int32, (1,))
     with _Device(dev) as stream:
         if out is None:
-            out = torch.empty(cols, n, device=dev)
-        else:
-            _matrix("out", out, dev, torch.float32, (cols, n))
-        size = C.c_size_t(0)
-        _ck(_lib.anakin_ckpt_weight_grad_workspace_bytes(DTYPES[dy.dtype], rows, cols, n, C.byref(size)))
-        ws = torch.empty(size.value, dtype=torch.uint8, device=dev)
-        _ck(_lib.anakin_ckpt_weight_grad(DTYPES[dy.dtype], a, rows, cols, n, _ptr(ck.codes), _ptr(ck.scales), _ptr(dy), ld, _ptr(out), _ld(out),
-                                         int(accumulate), _ptr(ws), ws.numel(), _ptr(status), stream))
+            out, ldw = torch.empty((cols, n), device=dev), n
+        size = _weight_grad_bytes(dt, rows, cols, n)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+        _ck(_lib.anakin_ckpt_weight_grad(dt, a, rows, cols, n, ck.codes.data_ptr(), ck.scales.data_ptr(), dy.data_ptr(), ld, out.data_ptr(), ldw,
+                                         int(accumulate), ws.data_ptr(), size, _vector("status", status, 1, dev, (torch.int32,)), stream))
     return out
