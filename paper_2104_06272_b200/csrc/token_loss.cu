@@ -59,7 +59,7 @@ Workspace carve(void* base, long long rows, long long sequences) {
     w.part = static_cast<double*>(take(sizeof(double) * kMaxPartials * kPolicyParts));
     w.per_seq = static_cast<int*>(take(sizeof(int) * (size_t)sequences));
     w.sums = static_cast<double*>(take(sizeof(double) * (size_t)sequences));
-    w.info = static_cast<int*>(take(sizeof(int) * (size_t)rows));
+    w.info = static_cast<int2*>(take(sizeof(int2) * (size_t)rows));
     w.bytes = off;
     return w;
 }
@@ -79,7 +79,7 @@ __device__ __forceinline__ void add_counts(bool counts, int seq, unsigned long l
     if (lane == __ffs(same) - 1 && atomicAdd(&per_seq[seq], __popc(same)) == 0) atomicAdd(seqs, 1ull);
 }
 
-__global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* per_seq, int* info) {
+__global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* per_seq, int2* info) {
     pdl_wait();  // (no early trigger: blocks of the next kernel placed around this one's would leave its clusters without room, a wave late)
     const long long stride = (long long)gridDim.x * 256;
     for (long long r0 = (long long)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < q.rows; r0 += stride) {
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* pe
         } else {
             seq = -2;
         }
-        if (info && r < q.rows) info[r] = seq;
+        if (info && r < q.rows) info[r] = make_int2(seq, q.tokens && seq > -2 ? (int)min(load_int(q.tokens, r, q.token_bytes), 0x7FFFFFFFll) : 0);
         if (c) add_counts(counts, seq, &c->rows, &c->sequences, per_seq);
     }
 }

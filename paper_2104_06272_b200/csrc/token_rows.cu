@@ -36,7 +36,7 @@ struct RowArgs {
     const float* ref;
     const Counts* counts;
     const int* per_seq;
-    const int* info;  // [rows] (k_token_counts)
+    const int2* info;  // [rows]: sequence and token (k_token_counts)
     double* part;
 };
 
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
         const bool there = r < q.rows;
         const T* x = static_cast<const T*>(q.logits) + (there ? r : 0) * q.ld;
         // (a row of no sequence has its log-probability, but no part in the loss)
-        const int info = !there ? -2 : MODE == FUSED ? A.info[r] : row_counts(q, r) ? 0 : -2;
+        const int info = !there ? -2 : MODE == FUSED ? A.info[r].x : row_counts(q, r) ? 0 : -2;
         const bool counts = info > -2, in_loss = info >= 0;
         const long long token = counts ? load_int(q.tokens, r, q.token_bytes) : 0;
         const int head = G >= 32 ? head_of<T>(x, V) : 0;
@@ -430,7 +430,8 @@ __device__ __forceinline__ void copies_but(int n) {
 // One warp more joins the sums: every warp's go into the shared memory of all blocks of the cluster (st.async, counted on an mbarrier; a cluster
 // barrier would also wait for the gradient's stores to memory), and while the others work on the next row it takes the token's terms of the
 // loss and leaves the row's constants for them.
-// The logits are read from memory once and their gradient written once.  8192 x 131072 bf16: 950 us, 4.5 TB/s.
+// The logits are read from memory once and their gradient written once.  8192 x 131072 bf16: 873 us, 4.9 TB/s (memory's share of it 654); issue slots and the
+// exponentials' unit are two thirds used.
 template <class T, int THREADS, int PER_SM, int MODE>
 __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideArgs W) {
     pdl_wait();
@@ -455,31 +456,39 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
     }
     tc::cluster_sync_all();
 
-    auto info_of = [&](long long r) -> int {  // sequence; -1: no part in the loss; -2: does not count
-        if (r >= q.rows) return -2;
+    // A row's sequence (-1: no part in the loss; -2: does not count) and its token, from 2^31 - 1 on cut off (no column is).
+    auto info_of = [&](long long r) -> int2 {
+        if (r >= q.rows) return make_int2(-2, 0);
         if (MODE == FUSED) return A.info[r];
-        return row_counts(q, r) ? 0 : -2;
+        return row_counts(q, r) ? make_int2(0, (int)min(load_int(q.tokens, r, q.token_bytes), 0x7FFFFFFFll)) : make_int2(-2, 0);
     };
-    auto token_of = [&](long long r, int of) -> long long { return of > -2 ? load_int(q.tokens, r, q.token_bytes) : 0; };
     const long long first = blockIdx.x / C;
     bool ok = true;  // no wait has given up; what follows one that has is NaN
 
     if (warp < WARPS) {
         const uint32_t mine = smem_of(held) + (uint32_t)tid * 16, other = (uint32_t)W.slice * 16;  // the second row's part
-        // of a row: this thread's first vector, and how far its vectors 0, THREADS, 2 THREADS, ... go
-        auto vectors = [&](long long r, const uint4*& p) -> int {
-            const T* x = static_cast<const T*>(q.logits) + r * q.ld;
-            const int head = head_of<T>(x, V);
-            p = reinterpret_cast<const uint4*>(x + head) + rank * W.slice + tid;
-            return min((V - head) / N - rank * W.slice, W.slice) - tid;
+        // Where a row's vectors of this thread begin, how far they (0, THREADS, 2 THREADS, ...) go, and the elements before the row's first vector.
+        struct Place {
+            const uint4* p;
+            int n, head;
         };
-        auto fetch = [&](long long r, int of, uint32_t at, int from) {  // vectors from the from-th on, in groups of U
-            const uint4* p = nullptr;
-            const int n = of > -2 ? vectors(r, p) : 0;
+        const unsigned char* ahead = static_cast<const unsigned char*>(q.logits) + first * q.ld * (long long)sizeof(T);  // the next row to be placed
+        const long long stride = (long long)clusters * q.ld * (long long)sizeof(T);
+        const int begin = rank * W.slice + tid;
+        auto place = [&]() -> Place {
+            Place w;
+            w.head = head_of<T>(ahead, V);
+            w.n = min((V - w.head) / N - rank * W.slice, W.slice) - tid;
+            w.p = reinterpret_cast<const uint4*>(ahead + w.head * (int)sizeof(T)) + begin;
+            ahead += stride;
+            return w;
+        };
+        auto fetch = [&](const Place& w, int of, uint32_t at, int from) {  // vectors from the from-th on, in groups of U
+            const int n = of > -2 ? w.n : 0;
             for (int i = from; i < n; i += U * THREADS) {
 #pragma unroll
                 for (int k = 0; k < U; ++k)
-                    if (i + k * THREADS < n) copy16_async(at + (uint32_t)(i + k * THREADS) * 16, p + i + k * THREADS);
+                    if (i + k * THREADS < n) copy16_async(at + (uint32_t)(i + k * THREADS) * 16, w.p + i + k * THREADS);
                 asm volatile("cp.async.commit_group;" ::: "memory");
             }
         };
@@ -489,16 +498,17 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
         };
         int sets = 0;  // rows whose sums have been sent
         // Maxima and sums of a row, to all blocks.
-        auto sums = [&](long long r, int of, long long token, uint32_t at) -> Row {
+        auto sums = [&](const Place& w, int of, int token, uint32_t at) -> Row {
             Row row = {0.f, INFINITY, -1};
-            if (r >= q.rows) return row;
-            const T* x = static_cast<const T*>(q.logits) + r * q.ld;
-            const int head = head_of<T>(x, V), nvec = (V - head) / N, tail = head + nvec * N;
-            const int n = min(nvec - rank * W.slice, W.slice) - tid;
-            if (rank == 0 && tid < head + V - tail) row.extra = tid < head ? tid : tail + tid - head;
+            const int n = w.n;
+            if (rank == 0) {
+                const int tail = w.head + (V - w.head) / N * N, e = tid < w.head ? tid : tail + tid - w.head;
+                if (e < V) row.extra = e;
+            }
             if (of <= -2) return row;
+            if (row.extra >= 0) row.xe = to_f(*(reinterpret_cast<const T*>(w.p - begin) - w.head + row.extra));
             float top = -INFINITY;
-            if (row.extra >= 0) top = row.low = row.xe = to_f(x[row.extra]);
+            if (row.extra >= 0) top = row.low = row.xe;
             const int groups = (n + U * THREADS - 1) / (U * THREADS);  // (n <= 0: none)
             int i = 0;
             for (int k = 1; i + (U - 1) * THREADS < n; i += U * THREADS, ++k) {
@@ -543,30 +553,30 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
                 acc.add(f, -INFINITY, c);
             }
             // the token's logit goes with its owner's sums (-inf from everybody else)
-            const int rel = (int)token - head - (rank * W.slice + tid) * N, vec = rel >= 0 ? rel / N : -1;
+            const int rel = token - w.head, vec = (rel >> (sizeof(T) == 4 ? 2 : 3)) - begin;  // (rel < 0: vec < 0)
             float xt = -INFINITY;
             bool own = false;
-            if (token < V) {
-                if (vec >= 0 && vec < n && vec % THREADS == 0) {
-                    own = true;
-                    T e;
-                    if constexpr (sizeof(T) == 4) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(e) : "r"(at + (uint32_t)vec * 16 + (uint32_t)(rel % N) * 4) : "memory");
-                    else {
-                        uint16_t w;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(at + (uint32_t)vec * 16 + (uint32_t)(rel % N) * 2) : "memory");
-                        e = *reinterpret_cast<T*>(&w);
-                    }
-                    xt = to_f(e);
-                } else if (row.extra >= 0 && row.extra == (int)token) {
-                    own = true;
-                    xt = row.xe;
+            if (vec >= 0 && vec < n && vec % THREADS == 0 && token < V) {
+                own = true;
+                if constexpr (sizeof(T) == 4) {
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(xt) : "r"(at + (uint32_t)vec * 16 + (uint32_t)(rel % N) * 4) : "memory");
+                } else {
+                    uint16_t h;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at + (uint32_t)vec * 16 + (uint32_t)(rel % N) * 2) : "memory");
+                    xt = to_f(*reinterpret_cast<const T*>(&h));
                 }
+            } else if (row.extra >= 0 && row.extra == token) {
+                own = true;
+                xt = row.xe;
             }
             const unsigned owner = __ballot_sync(0xFFFFFFFFu, own);
             if (owner) xt = __shfl_sync(0xFFFFFFFFu, xt, __ffs(owner) - 1);
             Soft v = acc.sums();
-            v.s = warp_sum(v.s);
-            v.t = warp_sum(v.t);
+            F2 st = f2(v.s, v.t);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) st = add2(st, f2(__shfl_xor_sync(0xFFFFFFFFu, st.x, o), __shfl_xor_sync(0xFFFFFFFFu, st.y, o)));
+            v.s = st.x;
+            v.t = st.y;
             const int set = sets++ & (SETS - 1);
             if (lane < C) {  // lane k writes to block k of the cluster
                 const uint32_t dst = tc::mapa(smem_of(&parts[set][rank * WARPS + warp]), (uint32_t)lane), bar = tc::mapa(smem_of(&arrived[set]), (uint32_t)lane);
@@ -577,67 +587,71 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
             return row;
         };
 
-        int info = info_of(first), info_next = info_of(first + clusters);
-        fetch(first, info, mine, 0);
-        fetch(first + clusters, info_next, mine + other, 0);
-        long long token = token_of(first, info), token_next = token_of(first + clusters, info_next);
-        Row row = sums(first, info, token, mine);  // (waits for both rows)
+        int2 info_next = info_of(first + clusters);
+        const int2 info_first = info_of(first);
+        Place now = place(), next = place();
+        fetch(now, info_first.x, mine, 0);
+        fetch(next, info_next.x, mine + other, 0);
+        Row row = sums(now, info_first.x, info_first.y, mine);  // (waits for both rows)
+        unsigned char* out_row = static_cast<unsigned char*>(A.dlogits) + first * A.ld_out * (long long)sizeof(T);
         int k = 0;
         for (long long r = first; r < q.rows; r += clusters, ++k) {
             const uint32_t here = mine + (k & 1 ? other : 0u), there = mine + (k & 1 ? 0u : other);
-            const int info_third = info_of(r + 2ll * clusters);
-            const Row next = sums(r + clusters, info_next, token_next, there);
-            const long long token_third = token_of(r + 2ll * clusters, info_third);
-            const uint4* p3 = nullptr;
-            const int n3 = info_third > -2 ? vectors(r + 2ll * clusters, p3) : 0;
+            const int2 info_third = info_of(r + 2ll * clusters);
+            const Row row_next = sums(next, info_next.x, info_next.y, there);
+            const Place third = place();
+            const uint4* p3 = third.p;
+            const int n3 = info_third.x > -2 ? third.n : 0;
             int i = 0;
             ok = ok && tc::mbar_wait(&ready[k & 1], (k >> 1) & 1);
             if (MODE == FUSED) {
                 RowGrad g = row_grad[k & 1];
                 if (!ok) g.kind = 3;
-                const T* x = static_cast<const T*>(q.logits) + r * q.ld;
-                const int head = head_of<T>(x, V), n = min((V - head) / N - rank * W.slice, W.slice) - tid;
-                T* out = static_cast<T*>(A.dlogits) + r * A.ld_out;
-                T* part_out = out + head + (size_t)(rank * W.slice + tid) * N;
-                const int j0 = head + (rank * W.slice + tid) * N;
+                const int n = now.n;
+                T* out = reinterpret_cast<T*>(out_row);
+                T* part_out = out + now.head + (size_t)begin * N;
+                const int j0 = now.head + begin * N;
                 const bool vec = ((uintptr_t)part_out & 15) == 0;
-                if (g.kind == 0 && row.low > -kHuge && vec) {
+                const bool fast = g.kind == 0 && row.low > -kHuge && vec;
+                if (fast) {
                     const F2 cc = f2(c, c), oo = f2(-g.off, -g.off), aa = f2(g.a, g.a), bb = f2(g.b, g.b);
                     const int at = g.token - j0;  // the taken token, from this thread's first element on
+                    auto one = [&](int iv) {
+                        float f[N];
+                        unpack16(lds16(here + (uint32_t)iv * 16), f, (const T*)nullptr);
+#pragma unroll
+                        for (int u = 0; u < N; u += 2) {
+                            const F2 d = fma2(f2(f[u], f[u + 1]), cc, oo), e = f2(ex2(d.x), ex2(d.y)), y = mul2(e, fma2(bb, d, aa));
+                            f[u] = y.x;
+                            f[u + 1] = y.y;
+                        }
+                        if ((unsigned)(at - iv * N) < (unsigned)N) {
+#pragma unroll
+                            for (int u = 0; u < N; ++u)
+                                if (u == at - iv * N) f[u] += g.onehot;
+                        }
+                        *reinterpret_cast<uint4*>(part_out + (size_t)iv * N) = pack16(f, (const T*)nullptr);
+                        if (iv < n3) copy16_async(here + (uint32_t)iv * 16, p3 + iv);
+                    };
                     for (; i + (U - 1) * THREADS < n; i += U * THREADS) {
 #pragma unroll
-                        for (int v = 0; v < U; ++v) {
-                            const int iv = i + v * THREADS;
-                            float f[N];
-                            unpack16(lds16(here + (uint32_t)iv * 16), f, (const T*)nullptr);
-#pragma unroll
-                            for (int u = 0; u < N; u += 2) {
-                                const F2 d = fma2(f2(f[u], f[u + 1]), cc, oo), e = f2(ex2(d.x), ex2(d.y)), y = mul2(e, fma2(bb, d, aa));
-                                f[u] = y.x;
-                                f[u + 1] = y.y;
-                            }
-                            if ((unsigned)(at - iv * N) < (unsigned)N) {
-#pragma unroll
-                                for (int u = 0; u < N; ++u)
-                                    if (u == at - iv * N) f[u] += g.onehot;
-                            }
-                            *reinterpret_cast<uint4*>(part_out + (size_t)iv * N) = pack16(f, (const T*)nullptr);
-                            if (iv < n3) copy16_async(here + (uint32_t)iv * 16, p3 + iv);
-                        }
+                        for (int v = 0; v < U; ++v) one(i + v * THREADS);
                         asm volatile("cp.async.commit_group;" ::: "memory");
                     }
+                    for (; i < n; i += THREADS) one(i);
+                    asm volatile("cp.async.commit_group;" ::: "memory");  // (a group too many only makes sums() wait for more)
                 }
-                const int whole = i;
-                for (; i < n; i += THREADS) store_vector(part_out + (size_t)i * N, g.template vector<T>(lds16(here + (uint32_t)i * 16), j0 + i * N, row.low, c), vec);
-                i = whole;
+                for (int j = fast ? n : 0; j < n; j += THREADS) store_vector(part_out + (size_t)j * N, g.template vector<T>(lds16(here + (uint32_t)j * 16), j0 + j * N, row.low, c), vec);
                 if (row.extra >= 0) out[row.extra] = from_f<T>(g.scalar(row.xe, row.extra, c));
             }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&done[k & 1]);
-            fetch(r + 2ll * clusters, info_third, here, i);
-            row = next;
+            fetch(third, info_third.x, here, i);
+            now = next;
+            next = third;
+            row = row_next;
             info_next = info_third;
-            token_next = token_third;
+            out_row += (long long)clusters * A.ld_out * (long long)sizeof(T);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
@@ -653,16 +667,16 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
             }
             return m;
         };
-        int info = info_of(first), info_next = info_of(first + clusters), sets = 0, k = 0;
-        long long token = token_of(first, info);
-        Taken taken = taken_of(first, info);
+        int2 info_now = info_of(first), info_next = info_of(first + clusters);
+        int sets = 0, k = 0;
+        Taken taken = taken_of(first, info_now.x);
         float weight = A.o.inv_divisor;  // of a row, but for the rows of its sequence
         if (MODE == FUSED && A.o.mean != ANAKIN_MEAN_FIXED) weight = (float)(A.o.mean == ANAKIN_MEAN_TOKEN ? A.counts->rows : A.counts->sequences);
         double stat = 0.0;  // of lane i: the i-th sum
         for (long long r = first; r < q.rows; r += clusters, ++k) {
-            const int info_third = info_of(r + 2ll * clusters);
-            const long long token_next = token_of(r + clusters, info_next);
-            const Taken taken_next = taken_of(r + clusters, info_next);
+            const int info = info_now.x, token = info_now.y;
+            const int2 info_third = info_of(r + 2ll * clusters);
+            const Taken taken_next = taken_of(r + clusters, info_next.x);
             float l = 0.f, H = 0.f, ls = 0.f, m = 0.f;
             RowGrad g = {0.f, 0.f, 0.f, 0.f, 0, 2};
             if (info > -2) {
@@ -715,9 +729,8 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
                     A.norm[2 * r + 1] = ls;
                 }
             }
-            info = info_next;
+            info_now = info_next;
             info_next = info_third;
-            token = token_next;
             taken = taken_next;
         }
         if (MODE == FUSED && rank == 0 && lane < kPolicyParts) A.part[(size_t)(blockIdx.x / C) * kPolicyParts + lane] = stat;
@@ -740,11 +753,12 @@ WidePlan wide_plan(const Rows& q, size_t es) {
         p.threads = bytes <= 6144 ? 64 : 128;
         return p;
     }
-    // two rows' parts a block: 35 KB each with three blocks of 288 threads an SM, 54 KB with two of 416, 110 KB with one of 544
+    // Two rows' parts a block: 54 KB each with two blocks an SM (three up to 35 KB: 16384 x 32000 bf16 471 us, with two 506), 110 KB with one.  Large
+    // parts, as every row costs every thread some 250 instructions besides its vectors (8192 x 131072 bf16 in clusters of 5 873 us, of 8 948).
     auto blocks = [&](long long most) { return (int)((vecs * 16 + most - 1) / most); };
-    const int a = blocks(35840), b = blocks(54272), d = blocks(111616);
-    p.threads = a <= kMaxCluster && a == b ? 256 : b <= kMaxCluster ? 384 : d <= kMaxCluster ? 512 : 0;
-    p.C = p.threads == 256 ? a : p.threads == 384 ? b : d;
+    const int b = blocks(54272), d = blocks(111616);
+    p.threads = b <= kMaxCluster ? 256 : d <= kMaxCluster ? 512 : 0;
+    p.C = b <= kMaxCluster ? b : d;
     // few rows: more blocks a row
     while (p.threads != 0 && p.C * 2 <= kMaxCluster && q.rows * p.C < 148 * 2 && vecs / p.C > 512) {
         p.C *= 2;
@@ -820,8 +834,8 @@ cudaError_t launch_rows_t(const RowArgs& A, int* parts, cudaStream_t s) {
         const WidePlan p = wide_plan(A.q, sizeof(T));
         if (p.threads != 0 && (MODE == FUSED || (p.threads >= 256 && A.q.rows < 592))) {
             const WideArgs W = {A, p.C, p.slice};
-            if (p.threads == 256) return launch_wide<T, 256, 3, MODE>(W, parts, s);
-            if (p.threads == 384) return launch_wide<T, 384, 2, MODE>(W, parts, s);
+            if (p.threads == 256 && p.slice * 16 <= 35840) return launch_wide<T, 256, 3, MODE>(W, parts, s);
+            if (p.threads == 256) return launch_wide<T, 256, 2, MODE>(W, parts, s);
             if (p.threads == 512) return launch_wide<T, 512, 1, MODE>(W, parts, s);
             if constexpr (MODE == FUSED) return p.threads == 64 ? launch_wide<T, 64, 8, MODE>(W, parts, s) : launch_wide<T, 128, 5, MODE>(W, parts, s);
         }

@@ -173,7 +173,7 @@ struct Workspace {
     double* part;   // [kMaxPartials][kPolicyParts]
     int* per_seq;   // [sequences]
     double* sums;   // [sequences] of the preference loss
-    int* info;      // [rows] of the policy gradient: the row's sequence; -1: no part in the loss, -2: does not count at all
+    int2* info;     // [rows] of the policy gradient: the row's sequence (-1: no part in the loss, -2: does not count at all) and its token
     size_t bytes;
 };
 Workspace carve(void* base, long long rows, long long sequences);
