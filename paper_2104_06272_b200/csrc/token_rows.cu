@@ -96,14 +96,6 @@ struct Soft {
             m = to;
         }
     }
-    __device__ __forceinline__ void join(float m2, float s2, float t2, float c) {
-        Soft b{m2, s2, t2};
-        const float to = fmaxf(m, m2);
-        rescale(to, c);
-        b.rescale(to, c);
-        s += b.s;
-        t += b.t;
-    }
 };
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -115,6 +107,19 @@ __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
+}
+
+// Of a group of L neighbouring lanes, in all of them: the maximum first, then sums on one scale.
+template <int L> __device__ __forceinline__ void group_sum(Soft& v, float c) {
+    float top = v.m;
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    v.rescale(top, c);
+    F2 st = f2(v.s, v.t);
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) st = add2(st, f2(__shfl_xor_sync(0xFFFFFFFFu, st.x, o), __shfl_xor_sync(0xFFFFFFFFu, st.y, o)));
+    v.s = st.x;
+    v.t = st.y;
 }
 
 // The same for one thread, the sums two lanes each.
@@ -271,18 +276,19 @@ template <class T> __device__ __forceinline__ void store_vector(T* out, const ui
 }
 
 // A group of G threads works on one row: G <= 32 lanes of a warp, or the whole block.  Rows are read straight into registers; where the gradient
-// follows (FUSED, rows of up to 1 KB) the second reading comes from the caches.  Groups below a warp take a row element by element.
+// follows (FUSED, rows of up to 1 KB) the second reading comes from the caches.  A thread alone takes a row element by element.
 // Backward alone, few rows: gridDim.y blocks share a row.
 template <class T, int G, int MODE>
 __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
     pdl_wait();
-    __shared__ float red[3 * 8];
+    __shared__ float4 red[2][8];
     __shared__ double redd[8];
     constexpr int GROUPS = 256 / G, N = Vec<T>::N, U = 4;
     const Rows& q = A.q;
     const int lane = threadIdx.x % G, V = (int)q.vocab;
     const float c = q.scale * kLog2e;
     double part[kPolicyParts] = {0.0, 0.0, 0.0, 0.0, 0.0};
+    int flip = 0;
     // (whole groups of a warp go through the loop together: the shuffles take all lanes)
     for (long long r0 = (long long)blockIdx.x * GROUPS; r0 < q.rows; r0 += (long long)gridDim.x * GROUPS) {
         const long long r = r0 + threadIdx.x / G;
@@ -292,17 +298,17 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
         const int info = !there ? -2 : MODE == FUSED ? A.info[r].x : row_counts(q, r) ? 0 : -2;
         const bool counts = info > -2, in_loss = info >= 0;
         const long long token = counts ? load_int(q.tokens, r, q.token_bytes) : 0;
-        const int head = G >= 32 ? head_of<T>(x, V) : 0;
-        const int nvec = G >= 32 ? (V - head) / N : 0, tail = head + nvec * N;
+        const int head = G > 1 ? head_of<T>(x, V) : 0;
+        const int nvec = G > 1 ? (V - head) / N : 0, tail = head + nvec * N;
         const uint4* xv = reinterpret_cast<const uint4*>(x + head);
-        // one element of a row's head or tail a thread
-        const int extra = G >= 32 && lane < head + V - tail ? (lane < head ? lane : tail + lane - head) : -1;
+        // the elements of a row's head and tail: the e-th
+        auto extra = [&](int e) { return e < head ? e : tail + e - head; };
         RowGrad gr;
         if constexpr (MODE != BACKWARD) {
             Acc acc;
             acc.clear();
             if (counts) {
-                if constexpr (G >= 32) {
+                if constexpr (G > 1) {
                     int i = lane;
                     for (; i + (U - 1) * G < nvec; i += U * G) {
                         uint4 u[U];
@@ -314,33 +320,29 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                         const uint4 u[1] = {xv[i]};
                         acc.template add_vectors<T>(u, c);
                     }
-                    if (extra >= 0) {
-                        const float f[2] = {to_f(x[extra]), -INFINITY};
+                    for (int e = lane; extra(e) < V; e += G) {
+                        const float f[2] = {to_f(x[extra(e)]), -INFINITY};
                         acc.add_scalars(f, c);
                     }
                 } else {
-                    for (int j = lane; j < V; j += 8 * G) {
+                    for (int j = 0; j < V; j += 8) {
                         float f[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) f[k] = j + k * G < V ? to_f(x[j + k * G]) : -INFINITY;
+                        for (int k = 0; k < 8; ++k) f[k] = j + k < V ? to_f(x[j + k]) : -INFINITY;
                         acc.add_scalars(f, c);
                     }
                 }
             }
             Soft v = acc.sums();
-            constexpr int L = G < 32 ? G : 32;
-#pragma unroll
-            for (int o = L / 2; o > 0; o >>= 1) {
-                const float m2 = __shfl_xor_sync(0xFFFFFFFFu, v.m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, v.s, o), t2 = __shfl_xor_sync(0xFFFFFFFFu, v.t, o);
-                v.join(m2, s2, t2, c);
-            }
+            group_sum<(G < 32 ? G : 32)>(v, c);
             if constexpr (G > 32) {
-                const int w = threadIdx.x >> 5;
+                // (two sets: a warp may be a row ahead of one that still reads)
+                if ((threadIdx.x & 31) == 0) red[flip][threadIdx.x >> 5] = make_float4(v.m, v.s, v.t, 0.f);
                 __syncthreads();
-                if ((threadIdx.x & 31) == 0) { red[3 * w] = v.m; red[3 * w + 1] = v.s; red[3 * w + 2] = v.t; }
-                __syncthreads();
-                v = Soft{red[0], red[1], red[2]};
-                for (int i = 1; i < G / 32; ++i) v.join(red[3 * i], red[3 * i + 1], red[3 * i + 2], c);
+                const float4 p = red[flip][threadIdx.x & 7];
+                flip ^= 1;
+                v = Soft{p.x, p.y, p.z};
+                group_sum<8>(v, c);
             }
             const bool none = v.s == 0.f;  // a row of -inf alone
             const float ls = none ? INFINITY : logf(v.s), H = none ? 0.f : ls - kLn2 * (v.t / v.s);
@@ -375,8 +377,8 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
         if (MODE != FORWARD && there) {
             if (!in_loss) gr.kind = 2;
             T* out = static_cast<T*>(A.dlogits) + r * A.ld_out;
-            if constexpr (G < 32) {
-                for (int j = lane; j < V; j += G) out[j] = from_f<T>(gr.scalar(to_f(x[j]), j, c));
+            if constexpr (G == 1) {
+                for (int j = 0; j < V; ++j) out[j] = from_f<T>(gr.scalar(to_f(x[j]), j, c));
             } else {
                 const bool vec = ((uintptr_t)(out + head) & 15) == 0;
                 const int step = G * gridDim.y;
@@ -387,7 +389,7 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                     store_vector(out + head + (size_t)(i + step) * N, gr.template vector<T>(u1, head + (i + step) * N, c), vec);
                 }
                 if (i < nvec) store_vector(out + head + (size_t)i * N, gr.template vector<T>(xv[i], head + i * N, c), vec);
-                if (extra >= 0 && blockIdx.y == 0) out[extra] = from_f<T>(gr.scalar(to_f(x[extra]), extra, c));
+                for (int e = lane; blockIdx.y == 0 && extra(e) < V; e += G) out[extra(e)] = from_f<T>(gr.scalar(to_f(x[extra(e)]), extra(e), c));
             }
         }
     }
@@ -828,8 +830,8 @@ cudaError_t launch_rows(const RowArgs& A, int* parts, cudaStream_t s) {
 template <class T, int MODE>
 cudaError_t launch_rows_t(const RowArgs& A, int* parts, cudaStream_t s) {
     if (A.q.vocab <= 8) return launch_rows<T, 1, MODE>(A, parts, s);
-    if (A.q.vocab <= 128) return launch_rows<T, 8, MODE>(A, parts, s);
     const long long bytes = A.q.vocab * (long long)sizeof(T);
+    if (bytes <= 1024) return launch_rows<T, 8, MODE>(A, parts, s);
     if constexpr (MODE != BACKWARD) {
         const WidePlan p = wide_plan(A.q, sizeof(T));
         if (p.threads != 0 && (MODE == FUSED || (p.threads >= 256 && A.q.rows < 592))) {
@@ -840,8 +842,9 @@ cudaError_t launch_rows_t(const RowArgs& A, int* parts, cudaStream_t s) {
             if constexpr (MODE == FUSED) return p.threads == 64 ? launch_wide<T, 64, 8, MODE>(W, parts, s) : launch_wide<T, 128, 5, MODE>(W, parts, s);
         }
     }
-    // a warp a row while that gives every SM its fill of rows
-    if (MODE == FUSED || bytes <= 4096 || (bytes <= 16384 && A.q.rows >= 148 * 16)) return launch_rows<T, 32, MODE>(A, parts, s);
+    // a warp a row while that gives every SM its fill of rows, several times over where rows are long (forward: 32768 x 12000 bf16 153 us, by whole
+    // blocks 291; backward by blocks 260, by warps 281)
+    if (MODE == FUSED || bytes <= 4096 || (bytes <= 16384 && A.q.rows >= 148 * 16) || (MODE == FORWARD && bytes <= 65536 && A.q.rows >= 148 * 192)) return launch_rows<T, 32, MODE>(A, parts, s);
     if constexpr (MODE != FUSED) return launch_rows<T, 256, MODE>(A, parts, s);
     return cudaErrorNotSupported;
 }
