@@ -495,9 +495,10 @@ int anakin_ckpt_backward(int dtype, int act, int64_t rows, int64_t cols, const u
  * Weight gradient of a layer whose input is act(x): dw[cols][n] (+)= act(x)^T dy, x from its checkpoint, dy [rows][n] of `dtype`; fp32 sums.
  * act: identity or relu (their values are exact in the tensor cores' 16 bits; others are refused with ANAKIN_E_UNSUPPORTED_CFG: checkpoint the
  * activation's output instead).  accumulate != 0 adds to dw (micro-batches).  rows = 0 gives zeros.
+ * The workspace holds 16-bit terms of dy (none for bf16 with dy_aligned != 0: dy and its rows start on 16-byte boundaries) and partial sums.
  * Every wait inside is bounded; one that gives up sets the bit that anakin_status documents in *dev_status (i32, may be NULL; the caller zeroes it).
  */
-int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t n, size_t* bytes);
+int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t n, int dy_aligned, size_t* bytes);
 int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int64_t n, const uint8_t* codes, const uint8_t* scales,
                             const void* dy, int64_t lddy, float* dw, int64_t lddw, int accumulate, void* dev_workspace, size_t bytes,
                             int32_t* dev_status, void* cuda_stream);

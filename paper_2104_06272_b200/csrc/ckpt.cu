@@ -15,18 +15,6 @@ namespace {
 using tok::from_f;
 using tok::to_f;
 
-// n / d and n % d for n < 2^31 by a multiplication (d >= 1; Granlund and Montgomery 1994): q = (n mul) >> (32 + shift).
-struct FastDiv {
-    uint32_t d, mul, shift;
-    explicit FastDiv(uint32_t div = 1) : d(div) {
-        shift = 0;
-        while ((1ull << shift) < div) ++shift;
-        // ceil(2^(31 + shift) / d) < 2^32, error below 2^shift: exact for n < 2^31
-        mul = (uint32_t)(((1ull << (31 + shift)) + div - 1) / div);
-    }
-    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (uint32_t)(((unsigned long long)n * mul) >> (31 + shift)); }
-};
-
 struct Args {
     long long rows;  // of this launch
     int cols, blocks;

@@ -5,13 +5,20 @@
 // that a first kernel writes.  So every product is exact in the MMA and the sums are the only rounding.  Both operands have the contraction index r
 // as their slow index ("MN-major").
 //
-// One CTA owns a 128 x BN tile of dW and a range of rows, in chunks of 64 rows:
-//   warp 0       TMA: the 64 x 128 codes and the 64 x BN planes of dY (64 x 64 boxes, 128-byte swizzle) into a ring of stages
-//   warps 4-7    codes -> bf16 in the swizzled layout (a thread turns 8 codes of a row into 16 bytes; block scales are fetched a chunk ahead)
-//   warp 1       tcgen05.mma into one of two accumulators in tensor memory; commits free the stage
-//   warps 8-15   add a finished accumulator to sums in registers; at the end store the tile, or the partial tile of a split
+// A CTA, or a pair of CTAs whose tensor cores work as one, owns tiles of dW (128 x BN, or 256 x BN with a half of either operand in each CTA) and walks
+// over rows in chunks of 64:
+//   warp 0       TMA: the 64 x 128 codes and the planes of dY (64 x 64 boxes, 128-byte swizzle) into a ring of stages
+//   warps 4-11   two warpgroups turn codes into bf16 in the swizzled layout, a chunk each in turn (a thread makes 16 bytes of 8 codes of a row; block
+//                scales are fetched ahead)
+//   warp 1       (of a pair: the first CTA's) tcgen05.mma into one of two accumulators in tensor memory; commits free the stage
+//   warps 12-19  add a finished accumulator to sums in registers; behind a tile's last chunk store them
 // The tensor core's fp32 accumulation rounds toward zero, which biases long sums (about 5e-8 of the sum an MMA): an accumulator takes at most 32
 // MMAs (512 rows of one bf16 term) and the groups are added with round-to-nearest.
+// The chunks of all tiles, one tile after the other, are dealt out in equal runs, so that every SM has the same work; a tile that several runs share is
+// summed from partial tiles, in their order, by a last kernel.
+// What bounds it: shared memory.  A chunk of a lone CTA's 128 x 256 tile moves 112 KB there in the 512 cycles of its MMAs, a pair's 80 KB (dY's half is
+// fetched and read once by each).  TIME_WGRAD
+#include <algorithm>
 #include <cstring>
 
 #include "ckpt.cuh"
@@ -22,16 +29,17 @@ namespace anakin {
 namespace ckpt {
 namespace {
 
-template <int BN_, int P_>
+template <int BN_, int P_, bool PAIR>
 struct Cfg {
-    static constexpr int BN = BN_, P = P_, BM = 128, KC = 64;
+    static constexpr int BN = BN_, P = P_, KC = 64, CONVERT = P == 1 ? 3 : 2, THREADS = 128 * (3 + CONVERT);  // CONVERT: converting warpgroups
+    static constexpr int NB = PAIR ? BN / 2 : BN;  // columns of dY that a CTA holds
     static constexpr int BOX = 64 * 64 * 2;
-    static constexpr int A_BYTES = (BM / 64) * BOX, B_PLANE = (BN / 64) * BOX, CODES = KC * BM;
+    static constexpr int A_BYTES = 2 * BOX, B_PLANE = (NB / 64) * BOX, CODES = KC * 128;
     static constexpr int STAGE = A_BYTES + P * B_PLANE + CODES;
-    static constexpr int FIT = (232448 - 1024 - 256) / STAGE;
-    static constexpr int STAGES = FIT >= 4 ? 4 : FIT;
+    static constexpr int FIT = (232448 - 1024 - 512) / STAGE;
+    static constexpr int STAGES = FIT >= 6 ? 6 : FIT;
     static constexpr int GROUP = P == 1 ? 8 : P == 2 ? 4 : 2;  // chunks an accumulator takes: 32, 32 and 24 MMAs
-    static constexpr size_t SMEM = (size_t)STAGES * STAGE + 1024 + 256;
+    static constexpr size_t SMEM = (size_t)STAGES * STAGE + 1024 + 512;
 };
 
 struct Maps {
@@ -39,72 +47,130 @@ struct Maps {
 };
 struct Args {
     int R, K, N, blocks;
-    int chunks_per_split;
+    int tiles_m, chunks;           // tiles along k; chunks of a tile
+    long long run, total;          // chunks of a run, of all tiles
+    int per_tile, tiles;           // per_tile > 0: so many runs to each tile, all tiles' first ones first; 0: runs go on from one tile to the next
     const uint8_t* scales;
-    float* out;  // dW, or the partial tiles [split][K][N]
-    long long ld, split_stride;
-    int relu, add;
-    bool vec;  // rows of `out` start on 16-byte boundaries
+    float* out;                    // dW, or partial tiles: that of a tile's i-th run at i * part_stride.  16-byte aligned, ld and width multiples of 4
+    long long ld, part_stride;
+    int width, relu;
     int32_t* status;
 };
 
-template <int BN, int P>
-__global__ void __launch_bounds__(512, 1) k_ckpt_wgrad(const __grid_constant__ Maps maps, Args a) {
-    using C = Cfg<BN, P>;
-    constexpr int STAGES = C::STAGES, GROUP = C::GROUP;
+// A run: tile after tile, chunk after chunk; groups of chunks end with a tile, with the run, and after GROUP chunks.
+template <int GROUP>
+struct Walk {
+    int left, tile, chunk, in_group;
+    __device__ __forceinline__ Walk(const Args& a, long long begin, long long end) : left((int)(end - begin)), tile((int)(begin / a.chunks)), chunk((int)(begin % a.chunks)), in_group(0) {}
+    __device__ __forceinline__ bool tile_ends(const Args& a) const { return chunk == a.chunks - 1 || left == 1; }
+    __device__ __forceinline__ bool group_ends(const Args& a) const { return in_group == GROUP - 1 || tile_ends(a); }
+    __device__ __forceinline__ void next(const Args& a) {
+        in_group = group_ends(a) ? 0 : in_group + 1;
+        --left;
+        if (++chunk == a.chunks) { chunk = 0; ++tile; }
+    }
+    // To the last chunk of the group.
+    __device__ __forceinline__ void to_group_end(const Args& a) {
+        const int more = min(min(GROUP - 1 - in_group, a.chunks - 1 - chunk), left - 1);
+        chunk += more;
+        in_group += more;
+        left -= more;
+    }
+};
+
+template <int BN, int P, bool PAIR>
+__global__ void __launch_bounds__((Cfg<BN, P, PAIR>::THREADS), 1) k_ckpt_wgrad(const __grid_constant__ Maps maps, Args a) {
+    using C = Cfg<BN, P, PAIR>;
+    // A barrier of codes is waited on by one warpgroup, every time it is used: one that skipped a phase could take an older one for its own.  So there is one
+    // for each stage and warpgroup.
+    constexpr int RAWS = C::STAGES * C::CONVERT;
+    constexpr int STAGES = C::STAGES, GROUP = C::GROUP, NCTA = PAIR ? 2 : 1;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* base = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint64_t* raw = (uint64_t*)(base + STAGES * C::STAGE);  // TMA done
-    uint64_t* full = raw + STAGES;                          // operand A written
+    // raw: this CTA's codes (alone: and dY) have arrived; of a pair's first CTA: rawb: both halves of dY; full: operand A is written, in both
+    uint64_t* raw = (uint64_t*)(base + STAGES * C::STAGE);
+    uint64_t* rawb = raw + RAWS;
+    uint64_t* full = rawb + STAGES;
     uint64_t* empty = full + STAGES;
     uint64_t* accfull = empty + STAGES;
     uint64_t* accempty = accfull + 2;
     uint32_t* tmem_slot = (uint32_t*)(accempty + 2);
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
-    const int m0 = blockIdx.x * C::BM, n0 = blockIdx.y * BN;
-    const int total = (a.R + C::KC - 1) / C::KC;
-    const int c0 = min((int)blockIdx.z * a.chunks_per_split, total), nchunks = min(a.chunks_per_split, total - c0);
-    const int ngroups = (nchunks + GROUP - 1) / GROUP;
+    const int rank = PAIR ? (int)tc::cluster_ctarank() : 0;
+    const long long run = blockIdx.x / NCTA;
+    const long long begin = a.per_tile > 0 ? run % a.tiles * a.chunks + run / a.tiles * a.run : run * a.run;
+    const long long end = min(begin + a.run, a.per_tile > 0 ? (run % a.tiles + 1) * a.chunks : a.total);
+    auto row0 = [&](int tile) { return (tile % a.tiles_m) * (128 * NCTA) + rank * 128; };  // this CTA's first row of dW
+    auto col0 = [&](int tile) { return (tile / a.tiles_m) * BN; };
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&raw[s], 1); tc::mbar_init(&full[s], 128); tc::mbar_init(&empty[s], 1); }
-        for (int q = 0; q < 2; ++q) { tc::mbar_init(&accfull[q], 1); tc::mbar_init(&accempty[q], 256); }
+        for (int s = 0; s < STAGES; ++s) {
+            tc::mbar_init(&rawb[s], 1);
+            tc::mbar_init(&full[s], 128 * NCTA);
+            tc::mbar_init(&empty[s], 1);
+        }
+        for (int s = 0; s < RAWS; ++s) tc::mbar_init(&raw[s], 1);
+        for (int q = 0; q < 2; ++q) { tc::mbar_init(&accfull[q], 1); tc::mbar_init(&accempty[q], 256 * NCTA); }
         tc::mbar_fence_init();
         tc::prefetch_map(&maps.codes);
         tc::prefetch_map(&maps.b[0]);
     }
-    if (wid == 2) tc::tmem_alloc(tmem_slot, 2 * BN);
+    if (wid == 2) {
+        if (PAIR) tc::tmem_alloc_pair(tmem_slot, 2 * BN);
+        else tc::tmem_alloc(tmem_slot, 2 * BN);
+    }
     tc::tc_fence_before();
     __syncthreads();
+    if (PAIR) tc::cluster_sync_all();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     pdl_wait();
     bool ok = true;
+    // barriers that the pair's first CTA waits on, arrived at from both
+    auto arrive_first = [&](uint64_t* bar) {
+        if (PAIR) tc::mbar_arrive_remote_cta_release(tc::mapa(tc::smem_u32(bar), 0));
+        else tc::mbar_arrive(bar);
+    };
+    auto wait_both = [&](uint64_t* bar, uint32_t parity) { return PAIR ? tc::mbar_wait_cluster(bar, parity) : tc::mbar_wait(bar, parity); };
+    auto commit = [&](uint64_t* bar) {
+        if (PAIR) tc::umma_commit_pair(bar, 3);
+        else tc::umma_commit(bar);
+    };
 
     if (wid < 4) {
-        tc::regs_dec<48>();
+        tc::regs_dec<32>();
         if (wid == 0 && lane == 0) {
-            for (int c = 0; c < nchunks; ++c) {
-                const int s = c % STAGES, r0 = (c0 + c) * C::KC;
-                if (c >= STAGES) ok = tc::mbar_wait(&empty[s], ((c / STAGES) - 1) & 1);
+            Walk<GROUP> w(a, begin, end);
+            for (int u = 0; w.left > 0; ++u, w.next(a)) {
+                const int s = u % STAGES, r0 = w.chunk * C::KC;
+                if (u >= STAGES) ok = tc::mbar_wait_long(&empty[s], ((u / STAGES) - 1) & 1);
                 if (!ok) break;
                 unsigned char* st = base + s * C::STAGE;
-                tc::mbar_expect_tx(&raw[s], P * C::B_PLANE + C::CODES);
-                tc::tma_load_2d(st + C::A_BYTES + P * C::B_PLANE, &maps.codes, &raw[s], m0, r0);
+                uint64_t* codes = &raw[u % RAWS];
+                tc::mbar_expect_tx(codes, C::CODES + (PAIR ? 0 : P * C::B_PLANE));
+                if (PAIR && rank == 0) tc::mbar_expect_tx(&rawb[s], 2 * P * C::B_PLANE);
+                tc::tma_load_2d(st + C::A_BYTES + P * C::B_PLANE, &maps.codes, codes, row0(w.tile), r0);
+                const int n0 = col0(w.tile) + rank * C::NB;
 #pragma unroll
                 for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int bx = 0; bx < BN / 64; ++bx)
-                        tc::tma_load_2d(st + C::A_BYTES + p * C::B_PLANE + bx * C::BOX, &maps.b[p], &raw[s], n0 + 64 * bx, r0);
+                    for (int bx = 0; bx < C::NB / 64; ++bx) {
+                        unsigned char* dst = st + C::A_BYTES + p * C::B_PLANE + bx * C::BOX;
+                        if (PAIR) tc::tma_load_2d_pair(dst, &maps.b[p], tc::mapa(tc::smem_u32(&rawb[s]), 0), n0 + 64 * bx, r0);
+                        else tc::tma_load_2d(dst, &maps.b[p], codes, n0 + 64 * bx, r0);
+                    }
             }
             if (!ok && a.status) atomicOr(a.status, DEV_E_WAIT_TIMEOUT);
-        } else if (wid == 1) {
-            const uint32_t idesc = tc::umma_idesc<1>(C::BM, BN, true, true);
-            for (int c = 0; c < nchunks; ++c) {
-                const int s = c % STAGES, grp = c / GROUP, cg = c - grp * GROUP;
+        } else if (wid == 1 && rank == 0) {
+            const uint32_t idesc = tc::umma_idesc<1>(128 * NCTA, BN, true, true);
+            int grp = 0;
+            Walk<GROUP> w(a, begin, end);
+            for (int u = 0; w.left > 0; ++u) {
+                const int s = u % STAGES;
                 const uint32_t acc = tmem + (uint32_t)((grp & 1) * BN);
-                if (cg == 0 && grp >= 2) ok = tc::mbar_wait(&accempty[grp & 1], ((grp >> 1) - 1) & 1);
-                ok = tc::warp_all(ok && tc::mbar_wait(&raw[s], (c / STAGES) & 1) && tc::mbar_wait(&full[s], (c / STAGES) & 1));
+                const bool first = w.in_group == 0, last = w.group_ends(a);
+                if (first && grp >= 2) ok = wait_both(&accempty[grp & 1], ((grp >> 1) - 1) & 1);
+                ok = tc::warp_all(ok && (PAIR ? tc::mbar_wait(&rawb[s], (u / STAGES) & 1) : tc::mbar_wait(&raw[u % RAWS], (u / RAWS) & 1)) && wait_both(&full[s], (u / STAGES) & 1));
                 if (!ok) break;
                 tc::tc_fence_after();
                 unsigned char* sa = base + s * C::STAGE;
@@ -113,178 +179,278 @@ __global__ void __launch_bounds__(512, 1) k_ckpt_wgrad(const __grid_constant__ M
 #pragma unroll
                     for (int p = P - 1; p >= 0; --p)  // (the small terms first)
 #pragma unroll
-                        for (int k16 = 0; k16 < C::KC / 16; ++k16)
-                            tc::umma(acc, tc::umma_desc(sa + k16 * 2048, C::BOX, 1024), tc::umma_desc(sb + p * C::B_PLANE + k16 * 2048, C::BOX, 1024), idesc,
-                                     (cg > 0 || k16 > 0 || p < P - 1) ? 1u : 0u);
-                    tc::umma_commit(&empty[s]);
-                    if (cg == GROUP - 1 || c == nchunks - 1) tc::umma_commit(&accfull[grp & 1]);
+                        for (int k16 = 0; k16 < C::KC / 16; ++k16) {
+                            const uint64_t ad = tc::umma_desc(sa + k16 * 2048, C::BOX, 1024), bd = tc::umma_desc(sb + p * C::B_PLANE + k16 * 2048, C::BOX, 1024);
+                            const uint32_t more = (!first || k16 > 0 || p < P - 1) ? 1u : 0u;
+                            if (PAIR) tc::umma_pair(acc, ad, bd, idesc, more);
+                            else tc::umma(acc, ad, bd, idesc, more);
+                        }
+                    commit(&empty[s]);
+                    if (last) commit(&accfull[grp & 1]);
                 }
                 __syncwarp();
+                if (last) ++grp;
+                w.next(a);
             }
             if (!ok && lane == 0 && a.status) atomicOr(a.status, DEV_E_WAIT_TIMEOUT);
         }
-    } else if (wid < 8) {
-        tc::regs_dec<96>();
-        const int t = tid - 128, ch = t & 15, rr = t >> 4;  // 8 columns from 8 ch on, of rows rr, rr + 8, ...
-        const int blk = (m0 >> 5) + (ch >> 2);
-        const bool col = blk < a.blocks;
-        const uint32_t dst0 = (uint32_t)((ch >> 3) * C::BOX + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4));  // (rr + 8 i) & 7 = rr & 7
-        uint32_t sc[8];
-        auto fetch = [&](int c) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = (c0 + c) * C::KC + rr + 8 * i;
-                sc[i] = col && c < nchunks && r < a.R ? (uint32_t)a.scales[(size_t)r * a.blocks + blk] : 0u;
-            }
+    } else if (wid < 4 + 4 * C::CONVERT) {
+        tc::regs_dec<C::CONVERT == 3 ? 40 : 64>();  // (launched with 80 or 96 a thread: 32 + 3 40 + 2 160 <= 6 80, 32 + 2 64 + 2 160 = 5 96)
+        constexpr int WGS = C::CONVERT;
+        const int wg = (wid >> 2) - 1;
+        // A thread has a row's 64 columns of one half of the tile: two scales, eight times 8 codes -> 16 bytes.  It takes them in the order j ^ g(row), g and
+        // row ^ g(row) both permutations of 0 .. 7 (twice and three times the row in GF(8); the second half's complemented): then neither the loads
+        // nor the swizzled stores of a warp meet in a bank.
+        const int row = (tid & 127) >> 1, half = tid & 1, r7 = row & 7, g = (((r7 << 1) ^ (r7 & 4 ? 11 : 0)) & 7) ^ (half ? 7 : 0);
+        const uint32_t src0 = (uint32_t)(C::A_BYTES + P * C::B_PLANE + row * 128 + half * 64 + g * 8), dst0 = (uint32_t)(half * C::BOX + row * 128 + ((g ^ r7) << 4));
+        const uint32_t relu = a.relu ? 0xFFFFFFFFu : 0u;
+        uint32_t sc0, sc1;  // of the first four in that order, and of the others
+        // This warpgroup's next chunk: its tile (and the block of columns in it that this thread begins with), its number in it, how many are left.
+        Walk<GROUP> w(a, begin, end);
+        int tile = w.tile, chunk = w.chunk, left = w.left, blk = 0;
+        auto skip = [&](int on) {
+            left -= on;
+            for (chunk += on; chunk >= a.chunks; chunk -= a.chunks) blk = (row0(++tile) >> 5) + 2 * half;
         };
-        fetch(0);
-        for (int c = 0; c < nchunks; ++c) {
-            const int s = c % STAGES;
+        blk = (row0(tile) >> 5) + 2 * half;
+        skip(wg);
+        auto fetch = [&]() {
+            const int r = chunk * C::KC + row, b0 = blk + (g >> 2), b1 = b0 ^ 1;  // (blk is even)
+            const uint8_t* p = a.scales + (size_t)r * a.blocks;
+            const bool in = left > 0 && r < a.R;
+            sc0 = in && b0 < a.blocks ? (uint32_t)p[b0] : 0u;
+            sc1 = in && b1 < a.blocks ? (uint32_t)p[b1] : 0u;
+        };
+        auto convert = [&](int u, int s) {
             // (a stage's last MMAs have finished before its codes were asked for: operand A may be written again)
-            ok = tc::mbar_wait(&raw[s], (c / STAGES) & 1);
-            if (!ok) break;
+            ok = tc::mbar_wait_long(&raw[u % RAWS], (u / RAWS) & 1);
+            if (!ok) return;
             unsigned char* st = base + s * C::STAGE;
-            const unsigned char* src = st + C::A_BYTES + P * C::B_PLANE + rr * 128 + ch * 8;
-            uint32_t now[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) now[i] = sc[i];
-            fetch(c + 1);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int j = 0; j < 8; ++j) {
+                uint2 q = *reinterpret_cast<const uint2*>(st + (src0 ^ (uint32_t)(j * 8)));
+                q = make_uint2(relu_codes(q.x, relu), relu_codes(q.y, relu));
                 float v[8];
-                decode8(*reinterpret_cast<const uint2*>(src + i * 1024), now[i], v);
-                if (a.relu) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = v[k] < 0.f ? 0.f : v[k];
-                }
-                *reinterpret_cast<uint4*>(st + dst0 + i * 1024) = tok::pack16(v, (const __nv_bfloat16*)nullptr);
+                decode8(q, j < 4 ? sc0 : sc1, v);
+                *reinterpret_cast<uint4*>(st + (dst0 ^ (uint32_t)(j * 16))) = tok::pack16(v, (const __nv_bfloat16*)nullptr);
             }
             tc::fence_proxy_async();
-            tc::mbar_arrive(&full[s]);
+            arrive_first(&full[s]);
+            skip(WGS);
+            fetch();
+        };
+        fetch();
+        for (int u = wg, s = wg % STAGES; left > 0 && ok; u += WGS) {
+            convert(u, s);
+            s += WGS;
+            if (s >= STAGES) s -= STAGES;
         }
         if (!ok && lane == 0 && a.status) atomicOr(a.status, DEV_E_WAIT_TIMEOUT);
     } else {
-        tc::regs_inc<184>();
+        tc::regs_inc<160>();
         constexpr int COLS = BN / 2;
-        const int q = wid & 3, half = (wid - 8) >> 2;
+        const int q = wid & 3, half = (wid >> 2) - 1 - C::CONVERT;
         float sum[COLS];
 #pragma unroll
         for (int j = 0; j < COLS; ++j) sum[j] = 0.f;
-        for (int grp = 0; grp < ngroups; ++grp) {
-            ok = tc::warp_all(tc::mbar_wait(&accfull[grp & 1], (grp >> 1) & 1));
-            if (!ok) break;
-            tc::tc_fence_after();
-            const uint32_t acc = tmem + (uint32_t)((grp & 1) * BN + half * COLS) + ((uint32_t)(32 * q) << 16);
+        int grp = 0;
+        for (Walk<GROUP> f(a, begin, end); f.left > 0; f.next(a)) {
+            f.to_group_end(a);
+            ok = tc::warp_all(ok && tc::mbar_wait_long(&accfull[grp & 1], (grp >> 1) & 1));
+            if (ok) {
+                tc::tc_fence_after();
+                const uint32_t acc = tmem + (uint32_t)((grp & 1) * BN + half * COLS) + ((uint32_t)(32 * q) << 16);
 #pragma unroll
-            for (int j0 = 0; j0 < COLS; j0 += 32) {
-                uint32_t r[32];
-                tc::tmem_ld32(acc + (uint32_t)j0, r);
+                for (int j0 = 0; j0 < COLS; j0 += 16) {
+                    uint32_t r[16];
+                    tc::tmem_ld16_nowait(acc + (uint32_t)j0, r);
+                    tc::tmem_ld_wait();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) sum[j0 + j] += __uint_as_float(r[j]);
-            }
-            tc::tc_fence_before();
-            if (grp + 2 < ngroups) tc::mbar_arrive(&accempty[grp & 1]);
-        }
-        if (!ok) {  // the caller sees it in the result, too
-            if (lane == 0 && a.status) atomicOr(a.status, DEV_E_WAIT_TIMEOUT);
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) sum[j] = NAN;
-        }
-        const int m = m0 + 32 * q + lane, nb = n0 + half * COLS;
-        if (m < a.K) {
-            float* dst = a.out + (size_t)blockIdx.z * a.split_stride + (size_t)m * a.ld + nb;
-#pragma unroll
-            for (int j = 0; j < COLS; j += 4) {
-                if (a.vec && nb + j + 4 <= a.N) {
-                    float4 v = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
-                    float4* p = reinterpret_cast<float4*>(dst + j);
-                    if (a.add) { const float4 o = *p; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
-                    *p = v;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (nb + j + i < a.N) dst[j + i] = a.add ? dst[j + i] + sum[j + i] : sum[j + i];
+                    for (int j = 0; j < 16; ++j) sum[j0 + j] += __uint_as_float(r[j]);
                 }
+                tc::tc_fence_before();
+                arrive_first(&accempty[grp & 1]);
+            }
+            ++grp;
+            if (f.tile_ends(a)) {
+                const int m = row0(f.tile) + 32 * q + lane, nb = col0(f.tile) + half * COLS;
+                // which of the tile's runs this is
+                const long long part = a.per_tile > 0 ? run / a.tiles : run - (long long)f.tile * a.chunks / a.run;
+                if (!ok) {  // the caller sees it in the result, too
+#pragma unroll
+                    for (int j = 0; j < COLS; ++j) sum[j] = NAN;
+                }
+                float4* dst = reinterpret_cast<float4*>(a.out + (size_t)part * a.part_stride + (size_t)m * a.ld + nb);
+                const int width = m < a.K ? a.width - nb : 0;
+#pragma unroll
+                for (int j = 0; j < COLS; j += 4)
+                    if (j < width) dst[j / 4] = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+#pragma unroll
+                for (int j = 0; j < COLS; ++j) sum[j] = 0.f;
             }
         }
+        if (!ok && lane == 0 && a.status) atomicOr(a.status, DEV_E_WAIT_TIMEOUT);
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (wid == 2) tc::tmem_dealloc(tmem, 2 * BN);
+    if (PAIR) tc::cluster_sync_all();
+    if (wid == 2) {
+        if (PAIR) tc::tmem_dealloc_pair(tmem, 2 * BN);
+        else tc::tmem_dealloc(tmem, 2 * BN);
+    }
 }
 
-// Partial tiles summed in the order of the splits.
-__global__ void __launch_bounds__(256) k_wgrad_sum(const float* part, int splits, long long stride, int K, int N, float* dw, long long ld, int add) {
+// Partial tiles summed in the order of the runs that left them; tile_k x tile_n each.
+__global__ void __launch_bounds__(256) k_wgrad_sum(const float* part, long long part_stride, int pitch, long long run, int per_tile, int chunks, int tiles_m, int tile_k, int tile_n, int K, int N,
+                                                   float* dw, long long ld, int add) {
     pdl_wait();
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)K * N; i += (long long)gridDim.x * 256) {
-        const long long k = i / N, n = i - k * N;
+        const int k = (int)(i / N), n = (int)(i - (long long)k * N);
+        int parts = 0;
+        if (chunks > 0) {
+            const long long t = (long long)(n / tile_n) * tiles_m + k / tile_k;
+            parts = per_tile > 0 ? per_tile : (int)((t * chunks + chunks - 1) / run - t * chunks / run) + 1;
+        }
         float v = 0.f;
-        for (int s = 0; s < splits; ++s) v += part[(size_t)s * stride + i];
+        for (int s = 0; s < parts; ++s) v += part[(size_t)s * part_stride + (size_t)k * pitch + n];
         float* p = dw + k * ld + n;
         *p = add ? *p + v : v;
     }
 }
 
-// dY as P bf16 planes [rows][pitch] that sum to it (fp32: 24 bits in three; fp16: 11 bits in two; bf16 whose rows TMA cannot address: one).
-template <class T, int P>
-__global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld, int R, int N, int pitch, __nv_bfloat16* planes, long long plane) {
+// dY as P bf16 planes [rows][pitch] that sum to it (fp32: 24 bits in three; fp16: 11 bits in two; bf16 whose rows TMA cannot address: one).  A thread
+// takes E neighbouring elements: 8 where rows start on 16-byte boundaries, else 2, so that a warp's loads lie side by side.
+template <class T, int P, int E>
+__global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld, FastDiv per_row, uint32_t pieces, int N, int pitch, __nv_bfloat16* planes,
+                                                      long long plane) {
     pdl_wait();
-    const int per_row = pitch / 8;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)R * per_row; i += (long long)gridDim.x * 256) {
-        const long long r = i / per_row;
-        const int j = (int)(i - r * per_row) * 8;
-        float v[8];
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += gridDim.x * 256) {
+        const uint32_t r = per_row.div(i);
+        const T* row = dy + (long long)r * ld;
+        const int j = (int)(i - r * per_row.d) * E;
+        float v[E];
+        if (E == 8 && j + E <= N) {
+            constexpr int V = 16 / sizeof(T);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = j + k < N ? tok::to_f(dy[r * ld + j + k]) : 0.f;
+            for (int k = 0; k < E; k += V) {
+                float f[V];
+                tok::unpack16(*reinterpret_cast<const uint4*>(row + j + k), f, (const T*)nullptr);
+#pragma unroll
+                for (int u = 0; u < V; ++u) v[k + u] = f[u];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) v[k] = j + k < N ? tok::to_f(row[j + k]) : 0.f;
+        }
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            float h[8];
+            uint32_t w[E / 2];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[k] = __bfloat162float(__float2bfloat16_rz(v[k]));  // (cut, not rounded: never past bf16's largest, and 8 bits a term are all 24)
-            *reinterpret_cast<uint4*>(planes + p * plane + r * pitch + j) = tok::pack16(h, (const __nv_bfloat16*)nullptr);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = fabsf(h[k]) < INFINITY ? v[k] - h[k] : 0.f;  // (an infinity stays one: its rest would be NaN)
+            for (int k = 0; k < E; k += 2) {
+                // (cut, not rounded: never past bf16's largest, and 8 bits a term are all 24)
+                const uint32_t a = v[k] == v[k] ? __float_as_uint(v[k]) & 0xFFFF0000u : 0x7FC00000u;
+                const uint32_t b = v[k + 1] == v[k + 1] ? __float_as_uint(v[k + 1]) & 0xFFFF0000u : 0x7FC00000u;
+                w[k / 2] = a >> 16 | b;
+                // (an infinity stays one: its rest would be NaN)
+                v[k] = fabsf(v[k]) < INFINITY ? v[k] - __uint_as_float(a) : 0.f;
+                v[k + 1] = fabsf(v[k + 1]) < INFINITY ? v[k + 1] - __uint_as_float(b) : 0.f;
+            }
+            __nv_bfloat16* out = planes + p * plane + (long long)r * pitch + j;
+            if constexpr (E == 8) *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint32_t*>(out) = w[0];
         }
     }
 }
 
 struct Plan {
-    int P, BN, pitch, splits, chunks_per_split;
-    bool direct;  // TMA reads the caller's dY
+    int P, BN, pitch, width, runs, per_tile, tiles_m, tiles, chunks, parts;  // parts: the most runs that share a tile; width: floats of a partial row
+    long long run, total;
+    bool direct, pair, straight;  // TMA reads the caller's dY; pairs of CTAs; the tiles are stored into dW
     size_t plane_bytes, part_off, bytes;
 };
 
-Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy, long long lddy) {
-    Plan p;
+Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy, long long lddy, const void* dw, long long lddw, bool add) {
+    Plan p = {};
     p.P = dtype == ANAKIN_DTYPE_F32 ? 3 : dtype == ANAKIN_DTYPE_F16 ? 2 : 1;
-    p.BN = N <= 64 ? 64 : N <= 128 || p.P > 1 ? 128 : 256;
+    p.pair = K > 128 && N > 64;  // (a pair's second CTA has the second 128 rows of dW)
+    p.BN = N <= 64 ? 64 : N <= 128 || (p.P > 1 && !p.pair) ? 128 : 256;
     p.direct = dtype == ANAKIN_DTYPE_BF16 && ((uintptr_t)dy & 15) == 0 && lddy % 8 == 0;
     p.pitch = (int)((N + 7) / 8 * 8);
     p.plane_bytes = ((size_t)R * p.pitch * 2 + 255) / 256 * 256;
-    const long long tiles = (K + 127) / 128 * ((N + p.BN - 1) / p.BN), chunks = (R + 63) / 64;
-    // as many splits as one wave holds, of at least four chunks each
-    long long splits = tiles < 148 ? 148 / tiles : 1;
-    if (splits > (chunks + 3) / 4) splits = (chunks + 3) / 4;
-    if (splits < 1) splits = 1;
-    p.chunks_per_split = (int)((chunks + splits - 1) / splits);
-    if (p.chunks_per_split < 1) p.chunks_per_split = 1;
-    p.splits = (int)((chunks + p.chunks_per_split - 1) / p.chunks_per_split);
+    const int tk = p.pair ? 256 : 128, most = p.pair ? 74 : 148;
+    p.tiles_m = (int)((K + tk - 1) / tk);
+    const long long tiles = p.tiles_m * ((N + p.BN - 1) / p.BN);
+    p.tiles = (int)tiles;  // (at most 2^15 times 2^16)
+    p.chunks = (int)((R + 63) / 64);
+    p.total = tiles * p.chunks;
+    // Either every tile gets the same number of runs: then all tiles' runs of the same rows are at work at one time and what they read comes from L2.
+    // Or runs of the same length go on from tile to tile and every SM is busy; then, where codes and dY are more than L2 holds, each tile reads its
+    // own from memory.  A run has four chunks at least; a chunk takes some 0.4 us (one term; 0.3 a term with more), a MB of partial sums written and
+    // read 0.25 us, a kernel or another wave of runs 2.
+    p.width = (int)((N + 3) / 4 * 4);
+    if (p.chunks == 0) return p;
+    const double us = p.P == 1 ? 0.4 : 0.3 * p.P, part_us = 1e-6 * (double)K * (double)N;
+    const double tiles_n = (double)((N + p.BN - 1) / p.BN), code_mb = 1e-6 * R * K, dy_mb = 2e-6 * R * N * p.P;
+    const long long most_each = std::max(1ll, std::min((p.chunks + 3ll) / 4, 3ll * most / tiles));
+    long long even = p.chunks;
+    double t_even = 1e30;
+    for (long long e = 1; e <= most_each; ++e) {
+        const long long len = (p.chunks + e - 1) / e, waves = (tiles * ((p.chunks + len - 1) / len) + most - 1) / most;
+        const double w = (double)waves * (us * (double)len + 2.0) + (e > 1 ? 2.0 + part_us * (double)(e + 1) : 0.0);
+        if (w < t_even) {
+            t_even = w;
+            even = len;
+        }
+    }
+    const long long each = (p.chunks + even - 1) / even;
+    long long flow = (p.total + most - 1) / most;
+    if (flow < 4) flow = 4;
+    const double read = (code_mb + dy_mb > 100.0 ? code_mb * tiles_n + dy_mb * p.tiles_m : code_mb + dy_mb) / 5.5;
+    const double t_flow = std::max(us * (double)flow, read) + 4.0 + part_us * 3.0;
+    if (t_even <= t_flow) {
+        p.per_tile = (int)each;
+        p.run = even;
+        p.parts = p.per_tile;
+        p.runs = tiles * each < (1ll << 30) && p.total < (1ll << 40) ? (int)(tiles * each) : 0;
+    } else {
+        p.run = flow;
+        p.parts = (int)((p.chunks + p.run - 2) / p.run) + 1;
+        p.runs = p.run < (1ll << 30) ? (int)((p.total + p.run - 1) / p.run) : 0;
+    }
     p.part_off = p.direct ? 0 : (size_t)p.P * p.plane_bytes;
-    p.bytes = p.part_off + (p.splits > 1 ? (size_t)p.splits * K * N * 4 : 0);
+    p.straight = R > 0 && p.parts == 1 && !add && ((uintptr_t)dw & 15) == 0 && lddw % 4 == 0 && N % 4 == 0;
+    p.bytes = p.part_off + (p.straight ? 0 : (size_t)p.parts * K * p.width * 4);
     return p;
 }
 
-template <int BN, int P>
+template <int BN, int P, bool PAIR>
 cudaError_t launch_wgrad(const Maps& maps, const Args& a, const Plan& p, cudaStream_t s) {
-    const dim3 grid((a.K + 127) / 128, (a.N + BN - 1) / BN, p.splits);
-    return launch<k_ckpt_wgrad<BN, P>>(grid, dim3(512), Cfg<BN, P>::SMEM, s, maps, a);
+    return launch_cluster<k_ckpt_wgrad<BN, P, PAIR>>(dim3(p.runs * (PAIR ? 2 : 1)), dim3(Cfg<BN, P, PAIR>::THREADS), Cfg<BN, P, PAIR>::SMEM, s, PAIR ? 2 : 1, maps, a);
+}
+template <int P>
+cudaError_t launch_wgrad_p(const Maps& maps, const Args& a, const Plan& p, cudaStream_t s) {
+    if (p.pair) return p.BN == 128 ? launch_wgrad<128, P, true>(maps, a, p, s) : launch_wgrad<256, P, true>(maps, a, p, s);
+    if constexpr (P == 1) {
+        if (p.BN == 256) return launch_wgrad<256, P, false>(maps, a, p, s);
+    }
+    return p.BN == 64 ? launch_wgrad<64, P, false>(maps, a, p, s) : launch_wgrad<128, P, false>(maps, a, p, s);
 }
 
 template <class T, int P>
 cudaError_t launch_split(const void* dy, long long ld, int R, int N, int pitch, void* ws, size_t plane_bytes, cudaStream_t s) {
-    const long long n = ((long long)R * (pitch / 8) + 255) / 256;
-    return launch<k_split_planes<T, P>>(dim3((unsigned)(n < 148 * 32 ? n : 148 * 32)), dim3(256), 0, s, static_cast<const T*>(dy), ld, R, N, pitch,
-                                        static_cast<__nv_bfloat16*>(ws), (long long)(plane_bytes / 2));
+    const bool vec = ((uintptr_t)dy & 15) == 0 && ld * sizeof(T) % 16 == 0;
+    const int per_row = pitch / (vec ? 8 : 2);
+    const long long most = ((1ll << 31) - 1) / per_row;  // rows of a launch: fewer than 2^31 pieces
+    for (long long r0 = 0; r0 < R; r0 += most) {
+        const uint32_t pieces = (uint32_t)(std::min(most, R - r0) * per_row), ctas = (pieces + 255) / 256;
+        const T* from = static_cast<const T*>(dy) + r0 * ld;
+        __nv_bfloat16* planes = static_cast<__nv_bfloat16*>(ws) + r0 * pitch;
+        const dim3 grid(std::min(ctas, 148u * 32));
+        const cudaError_t e = vec ? launch<k_split_planes<T, P, 8>>(grid, dim3(256), 0, s, from, ld, FastDiv((uint32_t)per_row), pieces, N, pitch, planes, (long long)(plane_bytes / 2))
+                                  : launch<k_split_planes<T, P, 2>>(grid, dim3(256), 0, s, from, ld, FastDiv((uint32_t)per_row), pieces, N, pitch, planes, (long long)(plane_bytes / 2));
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 int check_sizes(int dtype, int64_t rows, int64_t cols, int64_t n) {
@@ -302,11 +468,11 @@ using namespace anakin::ckpt;
 
 extern "C" {
 
-int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t n, size_t* bytes) {
+int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t n, int dy_aligned, size_t* bytes) {
     if (!bytes) return ANAKIN_E_INVALID_ARG;
     const int rc = check_sizes(dtype, rows, cols, n);
     if (rc != ANAKIN_OK) return rc;
-    *bytes = make_plan(dtype, rows, cols, n, (const void*)1, 1).bytes + 256;  // (for any address and stride of dy)
+    *bytes = make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8, nullptr, 1, true).bytes + 256;  // (for any dw)
     return ANAKIN_OK;
 }
 
@@ -321,12 +487,12 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
     if (lddy >= (int64_t(1) << 31) || lddw >= (int64_t(1) << 40)) return ANAKIN_E_INVALID_ARG;
     if (act != ANAKIN_ACT_IDENTITY && act != ANAKIN_ACT_RELU) return ANAKIN_E_UNSUPPORTED_CFG;
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
-    const Plan p = make_plan(dtype, rows, cols, n, dy, lddy);
+    const Plan p = make_plan(dtype, rows, cols, n, dy, lddy, dw, lddw, accumulate != 0);
+    if (rows > 0 && p.runs < 1) return ANAKIN_E_UNSUPPORTED_CFG;  // (months of work)
     if (bytes < p.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     const int K = (int)cols, N = (int)n, R = (int)rows;
     float* part = reinterpret_cast<float*>(static_cast<unsigned char*>(dev_workspace) + p.part_off);
-    const bool split = p.splits > 1 || rows == 0;
     if (rows > 0) {
         Maps maps;
         memset(&maps, 0, sizeof(maps));
@@ -346,25 +512,26 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
         a.R = R;
         a.K = K;
         a.N = N;
-        a.chunks_per_split = p.chunks_per_split;
+        a.tiles_m = p.tiles_m;
+        a.chunks = p.chunks;
+        a.run = p.run;
+        a.total = p.total;
+        a.per_tile = p.per_tile;
+        a.tiles = p.tiles;
         a.scales = scales;
-        a.out = split ? part : dw;
-        a.ld = split ? N : lddw;
-        a.split_stride = split ? (long long)K * N : 0;
+        a.out = p.straight ? dw : part;
+        a.ld = p.straight ? lddw : p.width;
+        a.part_stride = (long long)K * p.width;
+        a.width = p.width;
         a.relu = act == ANAKIN_ACT_RELU;
-        a.add = !split && accumulate;
-        a.vec = ((uintptr_t)a.out & 15) == 0 && a.ld % 4 == 0 && (!split || a.split_stride % 4 == 0);
         a.status = dev_status;
-        cudaError_t e;
-        if (p.P == 1) e = p.BN == 64 ? launch_wgrad<64, 1>(maps, a, p, s) : p.BN == 128 ? launch_wgrad<128, 1>(maps, a, p, s) : launch_wgrad<256, 1>(maps, a, p, s);
-        else if (p.P == 2) e = p.BN == 64 ? launch_wgrad<64, 2>(maps, a, p, s) : launch_wgrad<128, 2>(maps, a, p, s);
-        else e = p.BN == 64 ? launch_wgrad<64, 3>(maps, a, p, s) : launch_wgrad<128, 3>(maps, a, p, s);
+        const cudaError_t e = p.P == 1 ? launch_wgrad_p<1>(maps, a, p, s) : p.P == 2 ? launch_wgrad_p<2>(maps, a, p, s) : launch_wgrad_p<3>(maps, a, p, s);
         if (e != cudaSuccess) return tok::fail();
     }
-    if (split) {
+    if (!p.straight) {
         const long long ctas = ((long long)K * N + 255) / 256;
-        if (launch<k_wgrad_sum>(dim3((unsigned)(ctas < 148 * 32 ? ctas : 148 * 32)), dim3(256), 0, s, (const float*)part, rows == 0 ? 0 : p.splits, (long long)K * N, K, N,
-                                dw, (long long)lddw, accumulate) != cudaSuccess)
+        if (launch<k_wgrad_sum>(dim3((unsigned)(ctas < 148 * 32 ? ctas : 148 * 32)), dim3(256), 0, s, (const float*)part, (long long)K * p.width, p.width, p.run, p.per_tile, rows == 0 ? 0 : p.chunks,
+                                p.tiles_m, p.pair ? 256 : 128, p.BN, K, N, dw, (long long)lddw, accumulate) != cudaSuccess)
             return tok::fail();
     }
     return ANAKIN_OK;

@@ -38,6 +38,23 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, long l
     return false;
 }
 
+// The same for waits that are long as a rule: the thread is suspended for up to some 10 us at a time and leaves its issue slots to others.
+__device__ __forceinline__ bool mbar_wait_long(uint64_t* bar, uint32_t parity) {
+    const uint32_t addr = smem_u32(bar);
+    long long t0 = 0;
+    for (;;) {
+        uint32_t ok;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(ok)
+                     : "r"(addr), "r"(parity), "r"(10000)
+                     : "memory");
+        if (ok) return true;
+        const long long now = clock64();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 >= kWaitLimitClocks) return false;
+    }
+}
+
 // Shared-memory loads that the compiler may move ahead of earlier shared-memory stores (it cannot tell two parts of one shared array
 // apart, and a loop that loads, computes and stores then runs one trip at a time).  The address must have come through lds_base() after
 // the wait that makes the data readable, and what is loaded must go into a store, or anything else that stays in place, before the

@@ -53,7 +53,7 @@ _lib.anakin_ckpt_bytes.argtypes = [_i64, _i64, _sz, _sz]
 _lib.anakin_ckpt_forward.argtypes = [C.c_int, C.c_int, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp]
 _lib.anakin_ckpt_unpack.argtypes = [C.c_int, _i64, _i64, _vp, _vp, _vp, _i64, _vp]
 _lib.anakin_ckpt_backward.argtypes = [C.c_int, C.c_int, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp]
-_lib.anakin_ckpt_weight_grad_workspace_bytes.argtypes = [C.c_int, _i64, _i64, _i64, _sz]
+_lib.anakin_ckpt_weight_grad_workspace_bytes.argtypes = [C.c_int, _i64, _i64, _i64, C.c_int, _sz]
 _lib.anakin_ckpt_weight_grad.argtypes = [C.c_int, C.c_int, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _i64, C.c_int, _vp, C.c_size_t, _vp, _vp]
 
 
@@ -343,9 +343,9 @@ def ckpt_backward(ck: Checkpoint, dy: torch.Tensor, act: str = "relu", out: torc
 
 
 @functools.lru_cache(maxsize=256)
-def _weight_grad_bytes(dtype: int, rows: int, cols: int, n: int) -> int:
+def _weight_grad_bytes(dtype: int, rows: int, cols: int, n: int, aligned: bool) -> int:
     size = C.c_size_t(0)
-    _ck(_lib.anakin_ckpt_weight_grad_workspace_bytes(dtype, rows, cols, n, C.byref(size)))
+    _ck(_lib.anakin_ckpt_weight_grad_workspace_bytes(dtype, rows, cols, n, int(aligned), C.byref(size)))
     return size.value
 
 
@@ -367,8 +367,9 @@ def ckpt_weight_grad(ck: Checkpoint, dy: torch.Tensor, act: str = "identity", ou
     with _Device(dev) as stream:
         if out is None:
             out, ldw = torch.empty((cols, n), device=dev), n
-        size = _weight_grad_bytes(dt, rows, cols, n)
+        at = dy.data_ptr()
+        size = _weight_grad_bytes(dt, rows, cols, n, (at | ld * dy.element_size()) % 16 == 0)
         ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        _ck(_lib.anakin_ckpt_weight_grad(dt, a, rows, cols, n, ck.codes.data_ptr(), ck.scales.data_ptr(), dy.data_ptr(), ld, out.data_ptr(), ldw,
+        _ck(_lib.anakin_ckpt_weight_grad(dt, a, rows, cols, n, ck.codes.data_ptr(), ck.scales.data_ptr(), at, ld, out.data_ptr(), ldw,
                                          int(accumulate), ws.data_ptr(), size, _vector("status", status, 1, dev, (torch.int32,)), stream))
     return out

@@ -115,7 +115,7 @@ def test_checkpoint_refusals(tk):
     assert wg(dt=5) == wg(act=9) == wg(r=-1) == wg(c=0) == wg(k=0) == wg(q=None) == wg(dy=None) == wg(ld=7) == wg(dw=None) == wg(lddw=7) == wg(ws=None) == bad
     assert wg(dw=C.c_void_p(0x10002)) == wg(dy=C.c_void_p(0x10001)) == wg(ws=C.c_void_p(0x10010)) == wg(k=1 << 23) == bad
     assert wg(act=2) == wg(act=3) == -4 and wg(dt=0, r=4096, b=0) == -3
-    assert lib.anakin_ckpt_weight_grad_workspace_bytes(1, 4, 40, 8, None) == bad
+    assert lib.anakin_ckpt_weight_grad_workspace_bytes(1, 4, 40, 8, 1, None) == bad
 
 
 def test_host_tensors_are_refused(tk):
