@@ -29,52 +29,38 @@ struct Args {
     bool vec_x, vec_y;  // every row starts on a 16-byte boundary
 };
 
+// 1 / (1 + exp(-x)): 0 for x below -126 ln2 (there x times it is below 2^-119), NaN stays.
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + tok::ex2(-tok::kLog2e * x)); }
+// The normal distribution function and its density (times sqrt(2 pi)): 1 - Q(|x|) and the like with Hastings' rational approximation of erfc
+// (Abramowitz and Stegun 7.1.26: off by at most 1.5e-7), which needs the density's exponential and no branch.
+__device__ __forceinline__ float normal(float x, float& density) {
+    const float z = fabsf(x) * 0.70710678118654752f;
+    density = tok::ex2(-tok::kLog2e * z * z);
+    const float t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
+    const float q = 0.5f * density * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    return x > 0.f ? 1.f - q : q;
+}
 template <int ACT> __device__ __forceinline__ float act_of(float x) {
     if (ACT == ANAKIN_ACT_RELU) return x > 0.f ? x : x != x ? x : 0.f;
-    if (ACT == ANAKIN_ACT_SILU) return x / (1.f + expf(-x));
-    if (ACT == ANAKIN_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
+    if (ACT == ANAKIN_ACT_SILU) return x == -INFINITY ? 0.f : x * sigmoid(x);
+    if (ACT == ANAKIN_ACT_GELU) {
+        float d;
+        return x == -INFINITY ? 0.f : x * normal(x, d);
+    }
     return x;
 }
 template <int ACT> __device__ __forceinline__ float slope_of(float x) {
     if (ACT == ANAKIN_ACT_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
     if (ACT == ANAKIN_ACT_SILU) {
-        const float g = 1.f / (1.f + expf(-x));
-        return g * (1.f + x * (1.f - g));
+        const float g = sigmoid(x);
+        return fmaf(x * g, 1.f - g, g);
     }
-    if (ACT == ANAKIN_ACT_GELU) return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * 0.39894228040143268f * expf(-0.5f * x * x);
+    if (ACT == ANAKIN_ACT_GELU) {
+        float d;
+        const float n = normal(x, d);
+        return fmaf(x * 0.39894228040143268f, d, n);
+    }
     return 1.f;
-}
-
-// Eight columns of a row from column j on; what lies behind the row reads as zeros.
-template <class T> __device__ __forceinline__ void load8(const T* row, int j, int cols, bool vec, float (&f)[8]) {
-    if (vec && j + 8 <= cols) {
-        const uint4* p = reinterpret_cast<const uint4*>(row + j);
-        if constexpr (sizeof(T) == 4) {
-            const uint4 a = p[0], b = p[1];
-            f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
-            f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
-        } else {
-            tok::unpack16(p[0], f, (const T*)nullptr);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = j + i < cols ? to_f(row[j + i]) : 0.f;
-}
-template <class T> __device__ __forceinline__ void store8(T* row, int j, int cols, bool vec, const float (&f)[8]) {
-    if (vec && j + 8 <= cols) {
-        uint4* p = reinterpret_cast<uint4*>(row + j);
-        if constexpr (sizeof(T) == 4) {
-            p[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-            p[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
-        } else {
-            p[0] = tok::pack16(f, (const T*)nullptr);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (j + i < cols) row[j + i] = from_f<T>(f[i]);
 }
 
 // The smallest E in [-117, 120] with top 2^-E <= 448 = 1.75 2^8, from the bits of top (finite, >= 0).
@@ -85,13 +71,80 @@ __device__ __forceinline__ int exponent_of(float top) {
     return E < kMinExp ? kMinExp : E;  // (never above 120: e <= 127)
 }
 
+// A piece as it lies in memory: 16 bytes of a 16-bit type, 32 of fp32.
+template <class T> struct Raw { uint4 v[sizeof(T) / 2]; };
+template <class T> __device__ __forceinline__ Raw<T> load_raw(const T* row, int j, int cols, bool vec) {
+    Raw<T> r;
+    if (vec && j + 8 <= cols) {
+        const uint4* p = reinterpret_cast<const uint4*>(row + j);
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.v[k] = p[k];
+    } else {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = j + i < cols ? row[j + i] : from_f<T>(0.f);
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.v[k] = reinterpret_cast<const uint4*>(e)[k];
+    }
+    return r;
+}
+template <class T> __device__ __forceinline__ void store_raw(T* row, int j, int cols, bool vec, const Raw<T>& r) {
+    if (vec && j + 8 <= cols) {
+        uint4* p = reinterpret_cast<uint4*>(row + j);
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) p[k] = r.v[k];
+    } else {
+        T e[8];
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<uint4*>(e)[k] = r.v[k];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j + i < cols) row[j + i] = e[i];
+    }
+}
+template <class T> __device__ __forceinline__ void floats_of(const Raw<T>& r, float (&f)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+    } else {
+        tok::unpack16(r.v[0], f, (const T*)nullptr);
+    }
+}
+template <class T> __device__ __forceinline__ Raw<T> raw_of(const float (&f)[8]) {
+    Raw<T> r;
+    if constexpr (sizeof(T) == 4) {
+        r.v[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        r.v[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+    } else {
+        r.v[0] = tok::pack16(f, (const T*)nullptr);
+    }
+    return r;
+}
+// The largest |x| of a piece, infinities included, NaN passed over; 16-bit types two at a time.
+template <class T> __device__ __forceinline__ float largest(const Raw<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        float f[8], top = 0.f;
+        floats_of(r, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+        return top;
+    } else {
+        using P = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        auto abs2 = [](uint32_t w) { w &= 0x7FFF7FFFu; return *reinterpret_cast<const P*>(&w); };
+        const uint4& u = r.v[0];
+        const P m = __hmax2(__hmax2(abs2(u.x), abs2(u.y)), __hmax2(abs2(u.z), abs2(u.w)));
+        return fmaxf(fmaxf(to_f(m.x), to_f(m.y)), 0.f);
+    }
+}
+
 template <class T, int ACT>
 __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
     pdl_wait();
     constexpr int U = 2;
     // (a warp's lanes stay together: four of them share a block's largest value; `pieces` is a multiple of 4)
     for (uint32_t p0 = blockIdx.x * 256u * U + (threadIdx.x & ~31u); p0 < a.pieces; p0 += gridDim.x * 256u * U) {
-        float f[U][8];
+        Raw<T> x[U];
         uint32_t r[U], j[U];
         bool in[U];
 #pragma unroll
@@ -100,51 +153,57 @@ __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
             in[u] = p < a.pieces;
             r[u] = a.per_row.div(in[u] ? p : 0u);
             j[u] = ((in[u] ? p : 0u) - r[u] * a.per_row.d) * 8;
-            if (in[u]) load8(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, j[u], a.cols, a.vec_x, f[u]);
-            else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[u][i] = 0.f;
-            }
+            x[u] = load_raw(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, (int)j[u], a.cols, a.vec_x);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float top = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float v = fabsf(f[u][i]);
-                top = fmaxf(top, v < INFINITY ? v : 0.f);
-            }
+            float top = largest(x[u]), f[8];
+            floats_of(x[u], f);
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const bool odd = __any_sync(0xFFFFFFFFu, !(top < 2.6584559e36f));  // 2^121: an infinity in the block, or values near fp32's largest
+            if (odd) {  // the largest finite value
+                top = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.f);
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            }
             if (!in[u]) continue;
             const int E = exponent_of(top);
             const float down = __uint_as_float((uint32_t)(127 - E) << 23);  // 2^-E: E in [-117, 120]
             uint32_t w[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                uint32_t c = 0;
+                uint32_t c[2];
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const float x0 = f[u][4 * h + i], x1 = f[u][4 * h + i + 1];
-                    float v0 = x0 * down, v1 = x1 * down;
-                    if (E == kMaxExp) {  // (256 times 2^120 would be past the largest fp32 number)
-                        v0 = v0 > 240.f ? 240.f : v0 < -240.f ? -240.f : v0;
-                        v1 = v1 > 240.f ? 240.f : v1 < -240.f ? -240.f : v1;
+                for (int i = 0; i < 2; ++i) {
+                    const float x0 = f[4 * h + 2 * i], x1 = f[4 * h + 2 * i + 1];
+                    float2 v = __fmul2_rn(make_float2(x0, x1), make_float2(down, down));
+                    if (odd && E == kMaxExp) {  // (256 times 2^120 would be past the largest fp32 number)
+                        v.x = v.x > 240.f ? 240.f : v.x < -240.f ? -240.f : v.x;
+                        v.y = v.y > 240.f ? 240.f : v.y < -240.f ? -240.f : v.y;
                     }
-                    uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(v0, v1), __NV_SATFINITE, __NV_E4M3);
-                    if (!(fabsf(x0) < INFINITY)) b = (b & 0xFF00u) | 0x7Fu;
-                    if (!(fabsf(x1) < INFINITY)) b = (b & 0x00FFu) | 0x7F00u;
-                    c |= b << (8 * i);
+                    c[i] = __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);  // (NaN: 0x7F)
+                    if (odd) {
+                        if (!(fabsf(x0) < INFINITY)) c[i] = (c[i] & 0xFF00u) | 0x7Fu;
+                        if (!(fabsf(x1) < INFINITY)) c[i] = (c[i] & 0x00FFu) | 0x7F00u;
+                    }
                 }
-                w[h] = c;
+                w[h] = __byte_perm(c[0], c[1], 0x5410);
             }
             *reinterpret_cast<uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]) = make_uint2(w[0], w[1]);
             if ((threadIdx.x & 3) == 0) a.scales[(size_t)r[u] * a.blocks + j[u] / 32] = (uint8_t)(E + 127);
             if (a.y) {
-                float g[8];
+                T* row = static_cast<T*>(a.y) + (long long)r[u] * a.ldy;
+                if (ACT == ANAKIN_ACT_IDENTITY) {
+                    store_raw(row, (int)j[u], a.cols, a.vec_y, x[u]);
+                } else {
+                    float g[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = act_of<ACT>(f[u][i]);
-                store8(static_cast<T*>(a.y) + (long long)r[u] * a.ldy, j[u], a.cols, a.vec_y, g);
+                    for (int i = 0; i < 8; ++i) g[i] = act_of<ACT>(f[i]);
+                    store_raw(row, (int)j[u], a.cols, a.vec_y, raw_of<T>(g));
+                }
             }
         }
     }
@@ -153,14 +212,14 @@ __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
 template <class T> __device__ __forceinline__ float within(float v) { return v; }
 template <> __device__ __forceinline__ float within<__half>(float v) { return v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v; }
 
-// Unpack (BACK = false): y = the kept values; BACK: y = x act'(kept).
+// Unpack (BACK = false): y = the kept values; BACK: y = x act'(kept).  Four pieces of a thread in flight, with dy's 32 bytes of fp32 two.
 template <class T, int ACT, bool BACK>
 __global__ void __launch_bounds__(256) k_ckpt_read(Args a) {
     pdl_wait();
-    constexpr int U = 2;
+    constexpr int U = BACK && sizeof(T) == 4 ? 2 : 4;
     for (uint32_t p0 = blockIdx.x * 256u * U + threadIdx.x; p0 < a.pieces; p0 += gridDim.x * 256u * U) {
         uint2 c[U];
-        float d[U][8];
+        Raw<T> d[U];
         uint32_t r[U], j[U], s[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -170,16 +229,17 @@ __global__ void __launch_bounds__(256) k_ckpt_read(Args a) {
             j[u] = (p - r[u] * a.per_row.d) * 8;
             c[u] = *reinterpret_cast<const uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]);
             s[u] = a.scales[(size_t)r[u] * a.blocks + j[u] / 32];
-            if (BACK) load8(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, j[u], a.cols, a.vec_x, d[u]);
+            if (BACK) d[u] = load_raw(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, (int)j[u], a.cols, a.vec_x);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p0 + 256u * u >= a.pieces) continue;
-            float v[8];
+            float v[8], f[8];
             decode8(c[u], s[u], v);
+            if (BACK) floats_of(d[u], f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = BACK ? d[u][i] * slope_of<ACT>(v[i]) : within<T>(v[i]);
-            store8(static_cast<T*>(a.y) + (long long)r[u] * a.ldy, j[u], a.cols, a.vec_y, v);
+            for (int i = 0; i < 8; ++i) v[i] = BACK ? f[i] * slope_of<ACT>(v[i]) : within<T>(v[i]);
+            store_raw(static_cast<T*>(a.y) + (long long)r[u] * a.ldy, (int)j[u], a.cols, a.vec_y, raw_of<T>(v));
         }
     }
 }
