@@ -31,36 +31,49 @@ struct Args {
 
 // 1 / (1 + exp(-x)): 0 for x below -126 ln2 (there x times it is below 2^-119), NaN stays.
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + tok::ex2(-tok::kLog2e * x)); }
-// The normal distribution function and its density (times sqrt(2 pi)): 1 - Q(|x|) and the like with Hastings' rational approximation of erfc
-// (Abramowitz and Stegun 7.1.26: off by at most 1.5e-7), which needs the density's exponential and no branch.
-__device__ __forceinline__ float normal(float x, float& density) {
-    const float z = fabsf(x) * 0.70710678118654752f;
-    density = tok::ex2(-tok::kLog2e * z * z);
-    const float t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
-    const float q = 0.5f * density * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return x > 0.f ? 1.f - q : q;
+// The normal distribution function and its density (times sqrt(2 pi)) of two numbers: 1 - Q(|x|) and the like with Hastings' rational approximation of
+// erfc (Abramowitz and Stegun 7.1.26: off by at most 1.5e-7), which needs the density's exponential and no branch.
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 normal(float2 x, float2& density) {
+    const float2 z = __fmul2_rn(make_float2(fabsf(x.x), fabsf(x.y)), both(0.70710678118654752f));
+    const float2 e = __fmul2_rn(__fmul2_rn(z, z), both(-tok::kLog2e)), u = __ffma2_rn(z, both(0.3275911f), both(1.f));
+    density = make_float2(tok::ex2(e.x), tok::ex2(e.y));
+    const float2 t = make_float2(__fdividef(1.f, u.x), __fdividef(1.f, u.y));
+    float2 p = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    p = __ffma2_rn(t, p, both(0.5f * 1.421413741f));
+    p = __ffma2_rn(t, p, both(0.5f * -0.284496736f));
+    p = __ffma2_rn(t, p, both(0.5f * 0.254829592f));
+    const float2 q = __fmul2_rn(__fmul2_rn(density, t), p);
+    return make_float2(x.x > 0.f ? 1.f - q.x : q.x, x.y > 0.f ? 1.f - q.y : q.y);
 }
-template <int ACT> __device__ __forceinline__ float act_of(float x) {
-    if (ACT == ANAKIN_ACT_RELU) return x > 0.f ? x : x != x ? x : 0.f;
-    if (ACT == ANAKIN_ACT_SILU) return x == -INFINITY ? 0.f : x * sigmoid(x);
+template <int ACT> __device__ __forceinline__ float2 act_of(float2 x) {
+    auto one = [](float v) {
+        if (ACT == ANAKIN_ACT_RELU) return v > 0.f ? v : v != v ? v : 0.f;
+        if (ACT == ANAKIN_ACT_SILU) return v == -INFINITY ? 0.f : v * sigmoid(v);
+        return v;
+    };
     if (ACT == ANAKIN_ACT_GELU) {
-        float d;
-        return x == -INFINITY ? 0.f : x * normal(x, d);
+        float2 d;
+        const float2 y = __fmul2_rn(x, normal(x, d));
+        return make_float2(x.x == -INFINITY ? 0.f : y.x, x.y == -INFINITY ? 0.f : y.y);
     }
-    return x;
+    return make_float2(one(x.x), one(x.y));
 }
-template <int ACT> __device__ __forceinline__ float slope_of(float x) {
-    if (ACT == ANAKIN_ACT_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
-    if (ACT == ANAKIN_ACT_SILU) {
-        const float g = sigmoid(x);
-        return fmaf(x * g, 1.f - g, g);
-    }
+template <int ACT> __device__ __forceinline__ float2 slope_of(float2 x) {
+    auto one = [](float v) {
+        if (ACT == ANAKIN_ACT_RELU) return v > 0.f ? 1.f : v != v ? v : 0.f;
+        if (ACT == ANAKIN_ACT_SILU) {
+            const float g = sigmoid(v);
+            return fmaf(v * g, 1.f - g, g);
+        }
+        return 1.f;
+    };
     if (ACT == ANAKIN_ACT_GELU) {
-        float d;
-        const float n = normal(x, d);
-        return fmaf(x * 0.39894228040143268f, d, n);
+        float2 d;
+        const float2 n = normal(x, d);
+        return __ffma2_rn(__fmul2_rn(x, both(0.39894228040143268f)), d, n);
     }
-    return 1.f;
+    return make_float2(one(x.x), one(x.y));
 }
 
 // The smallest E in [-117, 120] with top 2^-E <= 448 = 1.75 2^8, from the bits of top (finite, >= 0).
@@ -73,33 +86,57 @@ __device__ __forceinline__ int exponent_of(float top) {
 
 // A piece as it lies in memory: 16 bytes of a 16-bit type, 32 of fp32.
 template <class T> struct Raw { uint4 v[sizeof(T) / 2]; };
-template <class T> __device__ __forceinline__ Raw<T> load_raw(const T* row, int j, int cols, bool vec) {
-    Raw<T> r;
-    if (vec && j + 8 <= cols) {
+// Eight columns of a row from column j on; what lies behind the row reads as zeros.
+template <class T> __device__ __forceinline__ Raw<T> load_piece(const void* base, long long ld, uint32_t r, uint32_t j, int cols, bool vec) {
+    const T* row = static_cast<const T*>(base) + (long long)r * ld;
+    Raw<T> x;
+    if (vec && (int)j + 8 <= cols) {
         const uint4* p = reinterpret_cast<const uint4*>(row + j);
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.v[k] = p[k];
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) x.v[k] = p[k];
     } else {
         T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = j + i < cols ? row[j + i] : from_f<T>(0.f);
+        for (int i = 0; i < 8; ++i) e[i] = (int)j + i < cols ? row[j + i] : from_f<T>(0.f);
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.v[k] = reinterpret_cast<const uint4*>(e)[k];
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) x.v[k] = reinterpret_cast<const uint4*>(e)[k];
     }
-    return r;
+    return x;
 }
-template <class T> __device__ __forceinline__ void store_raw(T* row, int j, int cols, bool vec, const Raw<T>& r) {
-    if (vec && j + 8 <= cols) {
-        uint4* p = reinterpret_cast<uint4*>(row + j);
+// The pieces of a warp's 32 lanes (none with in = false), all lanes together.  Where rows do not start on 16-byte boundaries (STAGED) they go element by
+// element, neighbouring lanes neighbouring elements, through 32 pieces of shared memory: a lane's own eight elements would touch sixteen
+// sectors a store instruction, a part of each (200000 x 777 bf16 unpacked: 445 us, this way 128; loads gain nothing by it).
+template <class T, bool STAGED>
+__device__ __forceinline__ void store_pieces(void* base, long long ld, uint32_t r, uint32_t j, bool in, int cols, T* stage, const Raw<T>& x) {
+    T* row = static_cast<T*>(base) + (long long)r * ld;
+    if constexpr (!STAGED) {
+        if (!in) return;
+        if ((int)j + 8 <= cols) {
+            uint4* p = reinterpret_cast<uint4*>(row + j);
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k) p[k] = r.v[k];
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) p[k] = x.v[k];
+        } else {
+            T e[8];
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<uint4*>(e)[k] = x.v[k];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((int)j + i < cols) row[j + i] = e[i];
+        }
     } else {
-        T e[8];
+        const int lane = threadIdx.x & 31, width = in ? min(cols - (int)j, 8) : 0;
+        T* to = row + j;
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<uint4*>(e)[k] = r.v[k];
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<uint4*>(stage)[lane * (sizeof(T) / 2) + k] = x.v[k];
+        __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (j + i < cols) row[j + i] = e[i];
+        for (int i = 0; i < 8; ++i) {  // elements 32 i + lane of the 256: of piece 4 i + lane / 8
+            const int src = 4 * i + (lane >> 3);
+            T* p = reinterpret_cast<T*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)to, src));
+            const int w = __shfl_sync(0xFFFFFFFFu, width, src);
+            if ((lane & 7) < w) p[lane & 7] = stage[32 * i + lane];
+        }
+        __syncwarp();
     }
 }
 template <class T> __device__ __forceinline__ void floats_of(const Raw<T>& r, float (&f)[8]) {
@@ -138,10 +175,12 @@ template <class T> __device__ __forceinline__ float largest(const Raw<T>& r) {
     }
 }
 
-template <class T, int ACT>
+template <class T, int ACT, bool STAGED>
 __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
     pdl_wait();
     constexpr int U = 2;
+    __shared__ __align__(16) T stages[STAGED ? 8 : 1][256];
+    T* stage = stages[STAGED ? threadIdx.x >> 5 : 0];
     // (a warp's lanes stay together: four of them share a block's largest value; `pieces` is a multiple of 4)
     for (uint32_t p0 = blockIdx.x * 256u * U + (threadIdx.x & ~31u); p0 < a.pieces; p0 += gridDim.x * 256u * U) {
         Raw<T> x[U];
@@ -153,7 +192,7 @@ __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
             in[u] = p < a.pieces;
             r[u] = a.per_row.div(in[u] ? p : 0u);
             j[u] = ((in[u] ? p : 0u) - r[u] * a.per_row.d) * 8;
-            x[u] = load_raw(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, (int)j[u], a.cols, a.vec_x);
+            x[u] = load_piece<T>(a.x, a.ldx, r[u], j[u], a.cols, a.vec_x);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -169,7 +208,6 @@ __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
                 top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             }
-            if (!in[u]) continue;
             const int E = exponent_of(top);
             const float down = __uint_as_float((uint32_t)(127 - E) << 23);  // 2^-E: E in [-117, 120]
             uint32_t w[2];
@@ -192,18 +230,22 @@ __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
                 }
                 w[h] = __byte_perm(c[0], c[1], 0x5410);
             }
-            *reinterpret_cast<uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]) = make_uint2(w[0], w[1]);
-            if ((threadIdx.x & 3) == 0) a.scales[(size_t)r[u] * a.blocks + j[u] / 32] = (uint8_t)(E + 127);
+            if (in[u]) {
+                *reinterpret_cast<uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]) = make_uint2(w[0], w[1]);
+                if ((threadIdx.x & 3) == 0) a.scales[(size_t)r[u] * a.blocks + j[u] / 32] = (uint8_t)(E + 127);
+            }
             if (a.y) {
-                T* row = static_cast<T*>(a.y) + (long long)r[u] * a.ldy;
-                if (ACT == ANAKIN_ACT_IDENTITY) {
-                    store_raw(row, (int)j[u], a.cols, a.vec_y, x[u]);
-                } else {
+                if (ACT != ANAKIN_ACT_IDENTITY) {
                     float g[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) g[i] = act_of<ACT>(f[i]);
-                    store_raw(row, (int)j[u], a.cols, a.vec_y, raw_of<T>(g));
+                    for (int i = 0; i < 8; i += 2) {
+                        const float2 v = act_of<ACT>(make_float2(f[i], f[i + 1]));
+                        g[i] = v.x;
+                        g[i + 1] = v.y;
+                    }
+                    x[u] = raw_of<T>(g);
                 }
+                store_pieces<T, STAGED>(a.y, a.ldy, r[u], j[u], in[u], a.cols, stage, x[u]);
             }
         }
     }
@@ -213,45 +255,60 @@ template <class T> __device__ __forceinline__ float within(float v) { return v; 
 template <> __device__ __forceinline__ float within<__half>(float v) { return v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v; }
 
 // Unpack (BACK = false): y = the kept values; BACK: y = x act'(kept).  Four pieces of a thread in flight, with dy's 32 bytes of fp32 two.
-template <class T, int ACT, bool BACK>
+template <class T, int ACT, bool BACK, bool STAGED>
 __global__ void __launch_bounds__(256) k_ckpt_read(Args a) {
     pdl_wait();
     constexpr int U = BACK && sizeof(T) == 4 ? 2 : 4;
-    for (uint32_t p0 = blockIdx.x * 256u * U + threadIdx.x; p0 < a.pieces; p0 += gridDim.x * 256u * U) {
+    __shared__ __align__(16) T stages[STAGED ? 8 : 1][256];
+    T* stage = stages[STAGED ? threadIdx.x >> 5 : 0];
+    for (uint32_t p0 = blockIdx.x * 256u * U + (threadIdx.x & ~31u); p0 < a.pieces; p0 += gridDim.x * 256u * U) {
         uint2 c[U];
         Raw<T> d[U];
         uint32_t r[U], j[U], s[U];
+        bool in[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t p = p0 + 256u * u;
-            if (p >= a.pieces) continue;
-            r[u] = a.per_row.div(p);
-            j[u] = (p - r[u] * a.per_row.d) * 8;
+            const uint32_t p = p0 + 256u * u + (threadIdx.x & 31);
+            in[u] = p < a.pieces;
+            r[u] = a.per_row.div(in[u] ? p : 0u);
+            j[u] = ((in[u] ? p : 0u) - r[u] * a.per_row.d) * 8;
             c[u] = *reinterpret_cast<const uint2*>(a.codes + (size_t)r[u] * a.blocks * 32 + j[u]);
             s[u] = a.scales[(size_t)r[u] * a.blocks + j[u] / 32];
-            if (BACK) d[u] = load_raw(static_cast<const T*>(a.x) + (long long)r[u] * a.ldx, (int)j[u], a.cols, a.vec_x);
+            if (BACK) d[u] = load_piece<T>(a.x, a.ldx, r[u], j[u], a.cols, a.vec_x);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (p0 + 256u * u >= a.pieces) continue;
             float v[8], f[8];
             decode8(c[u], s[u], v);
             if (BACK) floats_of(d[u], f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = BACK ? f[i] * slope_of<ACT>(v[i]) : within<T>(v[i]);
-            store_raw(static_cast<T*>(a.y) + (long long)r[u] * a.ldy, (int)j[u], a.cols, a.vec_y, raw_of<T>(v));
+            for (int i = 0; i < 8; i += 2) {
+                if (BACK) {
+                    const float2 g = __fmul2_rn(make_float2(f[i], f[i + 1]), slope_of<ACT>(make_float2(v[i], v[i + 1])));
+                    v[i] = g.x;
+                    v[i + 1] = g.y;
+                } else {
+                    v[i] = within<T>(v[i]);
+                    v[i + 1] = within<T>(v[i + 1]);
+                }
+            }
+            store_pieces<T, STAGED>(a.y, a.ldy, r[u], j[u], in[u], a.cols, stage, raw_of<T>(v));
         }
     }
 }
 
 enum { FORWARD = 0, UNPACK = 1, BACKWARD = 2 };
 
-template <class T, int ACT, int MODE>
-cudaError_t launch_one(const Args& a, cudaStream_t s) {
+template <class T, int ACT, int MODE, bool STAGED>
+cudaError_t launch_with(const Args& a, cudaStream_t s) {
     const uint32_t n = (a.pieces + 511) / 512;
     const dim3 grid(n < 148u * 32 ? n : 148u * 32);
-    if constexpr (MODE == FORWARD) return launch<k_ckpt_forward<T, ACT>>(grid, dim3(256), 0, s, a);
-    else return launch<k_ckpt_read<T, ACT, MODE == BACKWARD>>(grid, dim3(256), 0, s, a);
+    if constexpr (MODE == FORWARD) return launch<k_ckpt_forward<T, ACT, STAGED>>(grid, dim3(256), 0, s, a);
+    else return launch<k_ckpt_read<T, ACT, MODE == BACKWARD, STAGED>>(grid, dim3(256), 0, s, a);
+}
+template <class T, int ACT, int MODE>
+cudaError_t launch_one(const Args& a, cudaStream_t s) {
+    return a.y && !a.vec_y ? launch_with<T, ACT, MODE, true>(a, s) : launch_with<T, ACT, MODE, false>(a, s);
 }
 template <class T, int MODE>
 cudaError_t launch_act(int act, const Args& a, cudaStream_t s) {
