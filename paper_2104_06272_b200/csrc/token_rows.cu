@@ -282,7 +282,7 @@ template <class T, int G, int MODE>
 __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
     pdl_wait();
     __shared__ float4 red[2][8];
-    __shared__ double redd[8];
+    __shared__ double redd[8 * kPolicyParts];
     constexpr int GROUPS = 256 / G, N = Vec<T>::N, U = 4;
     const Rows& q = A.q;
     const int lane = threadIdx.x % G, V = (int)q.vocab;
@@ -394,10 +394,10 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
         }
     }
     if (MODE == FUSED) {
+        block_sums(part, redd);
+        if (threadIdx.x == 0) {
 #pragma unroll
-        for (int k = 0; k < kPolicyParts; ++k) {
-            const double s = block_sum(part[k], redd);
-            if (threadIdx.x == 0) A.part[(size_t)blockIdx.x * kPolicyParts + k] = s;
+            for (int k = 0; k < kPolicyParts; ++k) A.part[(size_t)blockIdx.x * kPolicyParts + k] = part[k];
         }
     }
 }

@@ -84,13 +84,13 @@ struct Rows {
 };
 
 // The sequence of row r: the last i with offsets[i] <= r; -1 before the first and `sequences` behind the last.  Any offsets give a
-// number in that range.
-__device__ __forceinline__ int sequence_of(const Rows& q, long long r) {
+// number in that range.  `near`: the offsets as 32-bit numbers in shared memory, or null.
+__device__ __forceinline__ int sequence_of(const Rows& q, long long r, const int* near = nullptr) {
     if (!q.offsets) return 0;
     int lo = 0, hi = q.sequences + 1;  // the number of offsets <= r lies in [lo, hi]
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (load_int(q.offsets, mid, q.offset_bytes) <= r) lo = mid + 1;
+        if ((near ? (long long)near[mid] : load_int(q.offsets, mid, q.offset_bytes)) <= r) lo = mid + 1;
         else hi = mid;
     }
     return lo - 1;
@@ -149,16 +149,26 @@ __device__ __forceinline__ float row_weight(const Objective& o, const Counts* c,
     return 1.f / ((float)per_seq[seq] * (float)c->sequences);
 }
 
-// Sum of v over the block's threads in a fixed order, in every thread; `red` holds a double for each warp.
-__device__ __forceinline__ double block_sum(double v, double* red) {
+// Sums of v[0 .. N-1] over the block's threads in a fixed order, in the threads of the first warp; `red` holds N doubles for each warp.
+template <int N> __device__ __forceinline__ void block_sums(double (&v)[N], double* red) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) red[(threadIdx.x >> 5) * N + k] = v[k];
+    }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double s = 0.0;
-    for (int i = 0; i < (int)(blockDim.x >> 5); ++i) s += red[i];
-    return s;
+    if (threadIdx.x < 32) {
+        const int warps = (int)(blockDim.x >> 5);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = (int)threadIdx.x < warps ? red[threadIdx.x * N + k] : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    }
 }
 
 // Rows of partial statistics, one for each CTA of a kernel, summed in order by one CTA (see token_loss.cu).
@@ -171,8 +181,9 @@ constexpr int kMaxPartials = 148 * 16;  // CTAs that may leave some
 struct Workspace {
     Counts* counts;
     double* part;   // [kMaxPartials][kPolicyParts]
-    int* per_seq;   // [sequences]
-    double* sums;   // [sequences] of the preference loss
+    int* per_seq;   // [sequences] (of the preference loss: times its splits)
+    double* sums;   // [sequences times splits] of the preference loss
+    float* coef;    // [sequences] of the preference loss
     int2* info;     // [rows] of the policy gradient: the row's sequence (-1: no part in the loss, -2: does not count at all) and its token
     size_t bytes;
 };

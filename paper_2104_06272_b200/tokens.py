@@ -113,53 +113,53 @@ def _ck(rc: int):
         raise AnakinError(rc)
 
 
-_F32 = torch.float32
+# The smallest of these calls cost the host more than the GPU, so the checks below are few attribute look-ups each.
+_F32, _U8, _Tensor, _empty = torch.float32, torch.uint8, torch.Tensor, torch.empty
 _TOKEN_ROWS = C.sizeof(TokenRows)
-_stream_of = torch._C._cuda_getCurrentRawStream  # the device's current stream as an integer
+_stream_of = torch._C._cuda_getCurrentRawStream  # a device's current stream as an integer
+_INTS, _FLAGS = (torch.int64, torch.int32), (torch.bool, torch.uint8)
 
 
 def _vector(name: str, t, n: int, dev: torch.device, dtypes=(_F32,)) -> int | None:
     """Address of t, a dense vector of n numbers on that device; None stays None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != 1 or t.shape[0] != n or t.device != dev or not t.is_contiguous():
+    if not isinstance(t, _Tensor) or t.dtype not in dtypes or t.shape != (n,) or t.device != dev or not t.is_contiguous():
         _refuse(f"{name}: a dense vector of {n} numbers ({', '.join(map(str, dtypes))}) on {dev} is needed")
     return t.data_ptr()
 
 
 def _matrix(name: str, t, dev=None, dtype=None, shape=None) -> tuple[int, int, int]:
     """(rows, cols, elements from row to row) of a matrix whose rows are dense."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype not in DTYPES or t.shape[1] < 1:
-        _refuse(f"{name}: a CUDA matrix of float32, bfloat16 or float16 with at least one column is needed")
-    rows, cols = t.shape
-    if (dev is not None and t.device != dev) or (dtype is not None and t.dtype is not dtype) or (shape is not None and (rows, cols) != shape):
-        _refuse(f"{name}: {dtype or 'a matrix'} of shape {shape} on {dev} is needed")
-    ld, step = t.stride()
-    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+    if not isinstance(t, _Tensor) or not t.is_cuda or t.dtype not in DTYPES or t.dim() != 2:
+        _refuse(f"{name}: a CUDA matrix of float32, bfloat16 or float16 is needed")
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if cols < 1 or (dev is not None and t.device != dev) or (dtype is not None and t.dtype is not dtype) or (shape is not None and (rows, cols) != shape):
+        _refuse(f"{name}: {dtype or 'a matrix'} of shape {shape or '(rows, one column at least)'} on {dev or 'a GPU'} is needed")
+    if rows <= 1:
+        ld = cols
+    if (cols > 1 and step != 1) or ld < cols:
         _refuse(f"{name}: columns have to lie side by side, and rows one after the other")
-    return rows, cols, ld if rows > 1 else cols
+    return rows, cols, ld
 
 
-class _Device:
-    """Makes the tensors' device current for the call and gives its current stream."""
-
-    __slots__ = ("index", "guard")
-
-    def __init__(self, dev: torch.device):
-        self.index, self.guard = dev.index, None
-
-    def __enter__(self) -> int:
-        if self.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-        return _stream_of(self.index)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_gpus = functools.lru_cache(maxsize=None)(torch.cuda.device_count)
 
 
-_INTS, _FLAGS = (torch.int64, torch.int32), (torch.bool, torch.uint8)
+def _on_its_device(call):
+    """The call with its tensors' GPU as the current one."""
+
+    @functools.wraps(call)
+    def wrapped(*args, **kw):
+        if _gpus() > 1:
+            for a in (*args, *kw.values()):
+                a = a.codes if isinstance(a, Checkpoint) else a
+                if isinstance(a, _Tensor) and a.is_cuda:
+                    with torch.cuda.device(a.device):
+                        return call(*args, **kw)
+        return call(*args, **kw)
+
+    return wrapped
 
 
 def _token_rows(dev, n, tokens, mask, offsets, logits=None, vocab=0, ld=0, scale=1.0) -> TokenRows:
@@ -172,7 +172,7 @@ def _token_rows(dev, n, tokens, mask, offsets, logits=None, vocab=0, ld=0, scale
     if mask is not None:
         r.mask = _vector("mask", mask, n, dev, _FLAGS)
     if offsets is not None:
-        count = offsets.numel() if isinstance(offsets, torch.Tensor) else 0
+        count = offsets.numel() if isinstance(offsets, _Tensor) else 0
         if count < 1:
             _refuse("offsets: one number more than there are sequences")
         r.offsets, r.offset_bytes, r.sequences = _vector("offsets", offsets, count, dev, _INTS), offsets.element_size(), count - 1
@@ -186,35 +186,30 @@ def _workspace_bytes(rows: int, sequences: int) -> int:
     return n.value
 
 
-def _floats(dev, *sizes: int) -> list[torch.Tensor]:
-    """Vectors of these lengths, one allocation (an allocation costs more than the smallest kernels)."""
-    return list(torch.empty(sum(sizes), device=dev).split(sizes))
-
-
 def _like(name: str, out, like: torch.Tensor) -> tuple[torch.Tensor, int]:
     """A matrix like `like`, and its elements from row to row."""
-    rows, cols = like.shape
     if out is None:
-        return torch.empty((rows, cols), dtype=like.dtype, device=like.device), cols
-    return out, _matrix(name, out, like.device, like.dtype, (rows, cols))[2]
+        if like.is_contiguous():
+            return torch.empty_like(like), like.shape[1]
+        return _empty(like.shape, dtype=like.dtype, device=like.device), like.shape[1]
+    return out, _matrix(name, out, like.device, like.dtype, tuple(like.shape))[2]
 
 
+@_on_its_device
 def logp(logits: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, mask: torch.Tensor | None = None, entropy: bool = True) -> TokenLogp:
     """Log-probability of every row's token under softmax(scale * logits), and the entropy (anakin_token_logp)."""
     n, vocab, ld = _matrix("logits", logits)
     dev = logits.device
     if tokens is None:
         _refuse("tokens are needed")
-    with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, None, logits, vocab, ld, scale)
-        if entropy:
-            norm, lp, ent = _floats(dev, 2 * n, n, n)
-        else:
-            (norm, lp), ent = _floats(dev, 2 * n, n), None
-        _ck(_lib.anakin_token_logp(rows, lp.data_ptr(), ent.data_ptr() if entropy else None, norm.data_ptr(), stream))
-    return TokenLogp(lp, ent, norm.view(n, 2))
+    stream = _stream_of(dev.index)
+    rows = _token_rows(dev, n, tokens, mask, None, logits, vocab, ld, scale)
+    norm, lp, ent = _empty(n, 2, device=dev), _empty(n, device=dev), _empty(n, device=dev) if entropy else None
+    _ck(_lib.anakin_token_logp(rows, lp.data_ptr(), ent.data_ptr() if entropy else None, norm.data_ptr(), stream))
+    return TokenLogp(lp, ent, norm)
 
 
+@_on_its_device
 def logp_backward(logits: torch.Tensor, tokens: torch.Tensor, norm: torch.Tensor, dlogp: torch.Tensor, entropy: torch.Tensor | None = None,
                   dentropy: torch.Tensor | None = None, scale: float = 1.0, mask: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient of the logits from those of logp and entropy (anakin_token_logp_backward).  norm and entropy come from logp() with the same
@@ -225,14 +220,15 @@ def logp_backward(logits: torch.Tensor, tokens: torch.Tensor, norm: torch.Tensor
         _refuse("tokens, norm and dlogp are needed, and entropy with dentropy")
     if _matrix("norm", norm, dev, _F32, (n, 2))[2] != 2:
         _refuse("norm: its rows lie one behind the other")
-    with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, None, logits, vocab, ld, scale)
-        out, ld_out = _like("out", out, logits)
-        _ck(_lib.anakin_token_logp_backward(rows, norm.data_ptr(), _vector("entropy", entropy, n, dev), _vector("dlogp", dlogp, n, dev),
-                                            _vector("dentropy", dentropy, n, dev), out.data_ptr(), ld_out, stream))
+    stream = _stream_of(dev.index)
+    rows = _token_rows(dev, n, tokens, mask, None, logits, vocab, ld, scale)
+    out, ld_out = _like("out", out, logits)
+    _ck(_lib.anakin_token_logp_backward(rows, norm.data_ptr(), _vector("entropy", entropy, n, dev), _vector("dlogp", dlogp, n, dev),
+                                        _vector("dentropy", dentropy, n, dev), out.data_ptr(), ld_out, stream))
     return out
 
 
+@_on_its_device
 def policy_loss(objective: PolicyObjective, logp: torch.Tensor, old_logp: torch.Tensor | None, adv: torch.Tensor, ref_logp: torch.Tensor | None = None,
                 entropy: torch.Tensor | None = None, mask: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
                 tokens: torch.Tensor | None = None) -> PolicyLoss:
@@ -242,20 +238,18 @@ def policy_loss(objective: PolicyObjective, logp: torch.Tensor, old_logp: torch.
     if adv is None or (objective.kl != 0 and ref_logp is None):
         _refuse("adv is needed, and ref_logp with a KL term")
     n, dev = logp.shape[0], logp.device
-    with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, offsets)
-        size = _workspace_bytes(n, rows.sequences)
-        ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        if entropy is not None:
-            stats, dlogp, dentropy = _floats(dev, len(POLICY_STATS), n, n)
-        else:
-            (stats, dlogp), dentropy = _floats(dev, len(POLICY_STATS), n), None
-        _ck(_lib.anakin_token_policy_loss(rows, objective, _vector("logp", logp, n, dev), _vector("old_logp", old_logp, n, dev), _vector("adv", adv, n, dev),
-                                          _vector("ref_logp", ref_logp, n, dev), _vector("entropy", entropy, n, dev), stats.data_ptr(), dlogp.data_ptr(),
-                                          None if dentropy is None else dentropy.data_ptr(), ws.data_ptr(), size, stream))
+    stream = _stream_of(dev.index)
+    rows = _token_rows(dev, n, tokens, mask, offsets)
+    size = _workspace_bytes(n, rows.sequences)
+    ws = _empty(size, dtype=_U8, device=dev)
+    stats, dlogp, dentropy = _empty(len(POLICY_STATS), device=dev), _empty(n, device=dev), _empty(n, device=dev) if entropy is not None else None
+    _ck(_lib.anakin_token_policy_loss(rows, objective, _vector("logp", logp, n, dev), _vector("old_logp", old_logp, n, dev), _vector("adv", adv, n, dev),
+                                      _vector("ref_logp", ref_logp, n, dev), _vector("entropy", entropy, n, dev), stats.data_ptr(), dlogp.data_ptr(),
+                                      None if dentropy is None else dentropy.data_ptr(), ws.data_ptr(), size, stream))
     return PolicyLoss(stats, dlogp, dentropy)
 
 
+@_on_its_device
 def policy_grad(objective: PolicyObjective, logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor | None, adv: torch.Tensor,
                 ref_logp: torch.Tensor | None = None, mask: torch.Tensor | None = None, offsets: torch.Tensor | None = None, scale: float = 1.0,
                 out: torch.Tensor | None = None) -> PolicyGrad:
@@ -264,18 +258,19 @@ def policy_grad(objective: PolicyObjective, logits: torch.Tensor, tokens: torch.
     dev = logits.device
     if tokens is None or adv is None or (objective.kl != 0 and ref_logp is None):
         _refuse("tokens and adv are needed, and ref_logp with a KL term")
-    with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, offsets, logits, vocab, ld, scale)
-        size = _workspace_bytes(n, rows.sequences)
-        ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        stats, lp, ent = _floats(dev, len(POLICY_STATS), n, n)
-        out, ld_out = _like("out", out, logits)
-        _ck(_lib.anakin_token_policy_grad(rows, objective, _vector("old_logp", old_logp, n, dev), _vector("adv", adv, n, dev),
-                                          _vector("ref_logp", ref_logp, n, dev), stats.data_ptr(), lp.data_ptr(), ent.data_ptr(), out.data_ptr(), ld_out,
-                                          ws.data_ptr(), size, stream))
+    stream = _stream_of(dev.index)
+    rows = _token_rows(dev, n, tokens, mask, offsets, logits, vocab, ld, scale)
+    size = _workspace_bytes(n, rows.sequences)
+    ws = _empty(size, dtype=_U8, device=dev)
+    stats, lp, ent = _empty(len(POLICY_STATS), device=dev), _empty(n, device=dev), _empty(n, device=dev)
+    out, ld_out = _like("out", out, logits)
+    _ck(_lib.anakin_token_policy_grad(rows, objective, _vector("old_logp", old_logp, n, dev), _vector("adv", adv, n, dev),
+                                      _vector("ref_logp", ref_logp, n, dev), stats.data_ptr(), lp.data_ptr(), ent.data_ptr(), out.data_ptr(), ld_out,
+                                      ws.data_ptr(), size, stream))
     return PolicyGrad(stats, lp, ent, out)
 
 
+@_on_its_device
 def preference_loss(objective: PreferenceObjective, logp: torch.Tensor, offsets: torch.Tensor, ref_logp: torch.Tensor | None = None,
                     mask: torch.Tensor | None = None, tokens: torch.Tensor | None = None) -> PreferenceLoss:
     """The preference loss over pairs of sequences, the preferred ones first, and its gradient (anakin_token_preference_loss)."""
@@ -284,40 +279,41 @@ def preference_loss(objective: PreferenceObjective, logp: torch.Tensor, offsets:
     if not isinstance(offsets, torch.Tensor) or offsets.numel() % 2 == 0:
         _refuse("offsets of an even number of sequences are needed")
     n, dev = logp.shape[0], logp.device
-    with _Device(dev) as stream:
-        rows = _token_rows(dev, n, tokens, mask, offsets)
-        size = _workspace_bytes(n, rows.sequences)
-        ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        stats, margin, dlogp = _floats(dev, len(PREFERENCE_STATS), rows.sequences // 2, n)
-        _ck(_lib.anakin_token_preference_loss(rows, objective, _vector("logp", logp, n, dev), _vector("ref_logp", ref_logp, n, dev), stats.data_ptr(),
-                                              margin.data_ptr(), dlogp.data_ptr(), ws.data_ptr(), size, stream))
+    stream = _stream_of(dev.index)
+    rows = _token_rows(dev, n, tokens, mask, offsets)
+    size = _workspace_bytes(n, rows.sequences)
+    ws = _empty(size, dtype=_U8, device=dev)
+    stats, margin, dlogp = _empty(len(PREFERENCE_STATS), device=dev), _empty(rows.sequences // 2, device=dev), _empty(n, device=dev)
+    _ck(_lib.anakin_token_preference_loss(rows, objective, _vector("logp", logp, n, dev), _vector("ref_logp", ref_logp, n, dev), stats.data_ptr(),
+                                          margin.data_ptr(), dlogp.data_ptr(), ws.data_ptr(), size, stream))
     return PreferenceLoss(stats, margin, dlogp)
 
 
 def _checkpoint(ck: Checkpoint) -> tuple[torch.device, int, int]:
     codes, scales, cols = ck
     blocks = (cols + 31) // 32
-    if cols < 1 or not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dtype is not torch.uint8 or codes.dim() != 2 or codes.shape[1] != blocks * 32 or \
-            not codes.is_contiguous():
+    if not isinstance(codes, _Tensor) or codes.dtype is not _U8 or not codes.is_cuda or codes.dim() != 2 or cols < 1 or codes.shape[1] != blocks * 32 or not codes.is_contiguous():
         _refuse(f"codes: a dense CUDA matrix of uint8 with {blocks * 32} columns is needed")
-    rows = codes.shape[0]
-    if not isinstance(scales, torch.Tensor) or scales.dtype is not torch.uint8 or scales.shape != (rows, blocks) or scales.device != codes.device or not scales.is_contiguous():
+    rows, dev = codes.shape[0], codes.device
+    if not isinstance(scales, _Tensor) or scales.dtype is not _U8 or scales.shape != (rows, blocks) or scales.device != dev or not scales.is_contiguous():
         _refuse(f"scales: a dense matrix of uint8, {rows} x {blocks}, is needed beside the codes")
-    return codes.device, rows, cols
+    return dev, rows, cols
 
 
+@_on_its_device
 def ckpt_forward(x: torch.Tensor, act: str = "relu", y: bool = True, out: torch.Tensor | None = None) -> tuple[torch.Tensor | None, Checkpoint]:
     """act(x) (None with y=False) and the checkpoint of x in 8 bits (anakin_ckpt_forward); `out` may be x itself."""
     rows, cols, ld = _matrix("x", x)
     a, dev, blocks = _one_of(ACTS, "act", act), x.device, (cols + 31) // 32
-    with _Device(dev) as stream:
-        res, ldy = _like("out", out, x) if y else (None, 0)
-        codes = torch.empty((rows, blocks * 32), dtype=torch.uint8, device=dev)
-        scales = torch.empty((rows, blocks), dtype=torch.uint8, device=dev)
-        _ck(_lib.anakin_ckpt_forward(DTYPES[x.dtype], a, rows, cols, x.data_ptr(), ld, res.data_ptr() if y else None, ldy, codes.data_ptr(), scales.data_ptr(), stream))
+    stream = _stream_of(dev.index)
+    res, ldy = _like("out", out, x) if y else (None, 0)
+    codes = _empty(rows, blocks * 32, dtype=_U8, device=dev)
+    scales = _empty(rows, blocks, dtype=_U8, device=dev)
+    _ck(_lib.anakin_ckpt_forward(DTYPES[x.dtype], a, rows, cols, x.data_ptr(), ld, res.data_ptr() if y else None, ldy, codes.data_ptr(), scales.data_ptr(), stream))
     return res, Checkpoint(codes, scales, cols)
 
 
+@_on_its_device
 def ckpt_unpack(ck: Checkpoint, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values that a checkpoint holds (anakin_ckpt_unpack)."""
     dev, rows, cols = _checkpoint(ck)
@@ -325,20 +321,21 @@ def ckpt_unpack(ck: Checkpoint, dtype: torch.dtype = torch.float32, out: torch.T
         ld, dtype = _matrix("out", out, dev, None, (rows, cols))[2], out.dtype
     elif dtype not in DTYPES:
         _refuse("float32, bfloat16 or float16")
-    with _Device(dev) as stream:
-        if out is None:
-            out, ld = torch.empty((rows, cols), dtype=dtype, device=dev), cols
-        _ck(_lib.anakin_ckpt_unpack(DTYPES[dtype], rows, cols, ck.codes.data_ptr(), ck.scales.data_ptr(), out.data_ptr(), ld, stream))
+    stream = _stream_of(dev.index)
+    if out is None:
+        out, ld = _empty(rows, cols, dtype=dtype, device=dev), cols
+    _ck(_lib.anakin_ckpt_unpack(DTYPES[dtype], rows, cols, ck.codes.data_ptr(), ck.scales.data_ptr(), out.data_ptr(), ld, stream))
     return out
 
 
+@_on_its_device
 def ckpt_backward(ck: Checkpoint, dy: torch.Tensor, act: str = "relu", out: torch.Tensor | None = None) -> torch.Tensor:
     """dy * act'(x) with x from its checkpoint (anakin_ckpt_backward); `out` may be dy itself."""
     dev, rows, cols = _checkpoint(ck)
     ld, a = _matrix("dy", dy, dev, None, (rows, cols))[2], _one_of(ACTS, "act", act)
-    with _Device(dev) as stream:
-        out, ldx = _like("out", out, dy)
-        _ck(_lib.anakin_ckpt_backward(DTYPES[dy.dtype], a, rows, cols, ck.codes.data_ptr(), ck.scales.data_ptr(), dy.data_ptr(), ld, out.data_ptr(), ldx, stream))
+    stream = _stream_of(dev.index)
+    out, ldx = _like("out", out, dy)
+    _ck(_lib.anakin_ckpt_backward(DTYPES[dy.dtype], a, rows, cols, ck.codes.data_ptr(), ck.scales.data_ptr(), dy.data_ptr(), ld, out.data_ptr(), ldx, stream))
     return out
 
 
@@ -349,6 +346,7 @@ def _weight_grad_bytes(dtype: int, rows: int, cols: int, n: int, aligned: bool) 
     return size.value
 
 
+@_on_its_device
 def ckpt_weight_grad(ck: Checkpoint, dy: torch.Tensor, act: str = "identity", out: torch.Tensor | None = None, accumulate: bool = False,
                      status: torch.Tensor | None = None) -> torch.Tensor:
     """act(x)^T dy, f32 [cols][n], with x from its checkpoint (anakin_ckpt_weight_grad); accumulate adds to `out`.  `status` (int32 [1], zeroed by
@@ -364,12 +362,12 @@ def ckpt_weight_grad(ck: Checkpoint, dy: torch.Tensor, act: str = "identity", ou
         ldw = _matrix("out", out, dev, _F32, (cols, n))[2]
     elif accumulate:
         _refuse("accumulate adds to `out`")
-    with _Device(dev) as stream:
-        if out is None:
-            out, ldw = torch.empty((cols, n), device=dev), n
-        at = dy.data_ptr()
-        size = _weight_grad_bytes(dt, rows, cols, n, (at | ld * dy.element_size()) % 16 == 0)
-        ws = torch.empty(size, dtype=torch.uint8, device=dev)
-        _ck(_lib.anakin_ckpt_weight_grad(dt, a, rows, cols, n, ck.codes.data_ptr(), ck.scales.data_ptr(), at, ld, out.data_ptr(), ldw,
-                                         int(accumulate), ws.data_ptr(), size, _vector("status", status, 1, dev, (torch.int32,)), stream))
+    stream = _stream_of(dev.index)
+    if out is None:
+        out, ldw = _empty(cols, n, device=dev), n
+    at = dy.data_ptr()
+    size = _weight_grad_bytes(dt, rows, cols, n, (at | ld * dy.element_size()) % 16 == 0)
+    ws = _empty(size, dtype=_U8, device=dev)
+    _ck(_lib.anakin_ckpt_weight_grad(dt, a, rows, cols, n, ck.codes.data_ptr(), ck.scales.data_ptr(), at, ld, out.data_ptr(), ldw,
+                                     int(accumulate), ws.data_ptr(), size, _vector("status", status, 1, dev, (torch.int32,)), stream))
     return out
