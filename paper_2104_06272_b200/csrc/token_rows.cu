@@ -190,16 +190,17 @@ struct Acc {
 // What the gradient of a row needs: 2^d ( a + b d ), d = c x - off or c (x - off), and `onehot` more at the token.
 struct RowGrad {
     float off, a, b, onehot;
-    int token, kind;  // kind: 0 usual, 1 = m is beyond 2^100, 2 = zeros, 3 = NaN
-    __device__ __forceinline__ void set(float m, float ln_s, float g, float h, float H, float scale, float c, long long tok, long long V) {
+    int token, kind;  // kind: 0 usual, 1 = from differences (m beyond 2^100, or a short row), 2 = zeros, 3 = NaN
+    __device__ __forceinline__ void set(float m, float ln_s, float g, float h, float H, float scale, float c, long long tok, long long V, bool as_differences = false) {
         const float ls2 = ln_s * kLog2e, inv = ex2(-ls2);
         const float a0 = -scale * (g + h * H), b0 = -scale * h * kLn2;  // p ( a0 + b0 log2 p ),  p = 2^d / s
         a = (a0 - b0 * ls2) * inv;
         b = b0 * inv;
         onehot = scale * g;
-        off = usual(m) ? __fmul_rn(m, c) : m;
+        const bool fused = usual(m) && !as_differences;
+        off = fused ? __fmul_rn(m, c) : m;
         token = (int)tok;
-        kind = tok >= V ? 3 : ln_s == INFINITY ? 2 : usual(m) ? 0 : 1;
+        kind = tok >= V ? 3 : ln_s == INFINITY ? 2 : fused ? 0 : 1;
     }
     template <int N> __device__ __forceinline__ void at(float (&f)[N], float low, float c) const {
         const F2 cc = f2(c, c), oo = f2(-off, -off), aa = f2(a, a), bb = f2(b, b);
@@ -264,6 +265,8 @@ template <class T> __device__ __forceinline__ int head_of(const void* p, long lo
     return (long long)h < n ? h : (int)n;
 }
 
+constexpr int kShortRow = 128;  // rows of up to so many logits are taken more exactly (see k_token_rows)
+
 template <class T> __device__ __forceinline__ void store_vector(T* out, const uint4& u, bool vec) {
     if (vec) {
         *reinterpret_cast<uint4*>(out) = u;
@@ -287,6 +290,7 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
     const Rows& q = A.q;
     const int lane = threadIdx.x % G, V = (int)q.vocab;
     const float c = q.scale * kLog2e;
+    const bool as_differences = G == 1 || (G <= 8 && V <= kShortRow);
     double part[kPolicyParts] = {0.0, 0.0, 0.0, 0.0, 0.0};
     int flip = 0;
     // (whole groups of a warp go through the loop together: the shuffles take all lanes)
@@ -307,7 +311,9 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
         if constexpr (MODE != BACKWARD) {
             Acc acc;
             acc.clear();
-            if (counts) {
+            if (counts && as_differences) {  // (only the maximum is needed here)
+                for (int j = lane; j < V; j += G) acc.m = fmaxf(acc.m, to_f(x[j]));
+            } else if (counts) {
                 if constexpr (G > 1) {
                     int i = lane;
                     for (; i + (U - 1) * G < nvec; i += U * G) {
@@ -324,31 +330,54 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                         const float f[2] = {to_f(x[extra(e)]), -INFINITY};
                         acc.add_scalars(f, c);
                     }
-                } else {
-                    for (int j = 0; j < V; j += 8) {
-                        float f[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) f[k] = j + k < V ? to_f(x[j + k]) : -INFINITY;
-                        acc.add_scalars(f, c);
-                    }
                 }
             }
             Soft v = acc.sums();
-            group_sum<(G < 32 ? G : 32)>(v, c);
-            if constexpr (G > 32) {
-                // (two sets: a warp may be a row ahead of one that still reads)
-                if ((threadIdx.x & 31) == 0) red[flip][threadIdx.x >> 5] = make_float4(v.m, v.s, v.t, 0.f);
-                __syncthreads();
-                const float4 p = red[flip][threadIdx.x & 7];
-                flip ^= 1;
-                v = Soft{p.x, p.y, p.z};
-                group_sum<8>(v, c);
+            float ls, H;
+            bool none;
+            if (as_differences) {
+                // Beside the largest logit the others may be next to nothing: s - 1 is summed, and ln s is its log1p.
+                float top = v.m, s = 0.f, t = 0.f, n = 0.f;
+#pragma unroll
+                for (int o = G / 2; o > 0; o >>= 1)
+                    if (G <= 8) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                for (int j = lane; counts && j < V; j += G) {
+                    const float f = to_f(x[j]), d = q.scale * (f - top), e = expf(d);
+                    if (f == top) n += 1.f;
+                    else {
+                        s += e;
+                        if (e != 0.f) t = fmaf(e, d, t);
+                    }
+                }
+#pragma unroll
+                for (int o = G / 2; o > 0; o >>= 1) {
+                    s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+                    t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+                    n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
+                }
+                none = top == -INFINITY && s == s;
+                if (top == INFINITY) s = NAN;
+                ls = none ? INFINITY : n == 1.f ? log1pf(s) : logf(n + s);
+                H = none ? 0.f : ls - t / (n + s);
+                v.m = top;
+            } else {
+                group_sum<(G < 32 ? G : 32)>(v, c);
+                if constexpr (G > 32) {
+                    // (two sets: a warp may be a row ahead of one that still reads)
+                    if ((threadIdx.x & 31) == 0) red[flip][threadIdx.x >> 5] = make_float4(v.m, v.s, v.t, 0.f);
+                    __syncthreads();
+                    const float4 p = red[flip][threadIdx.x & 7];
+                    flip ^= 1;
+                    v = Soft{p.x, p.y, p.z};
+                    group_sum<8>(v, c);
+                }
+                none = v.s == 0.f;  // a row of -inf alone
+                ls = none ? INFINITY : logf(v.s);
+                H = none ? 0.f : ls - kLn2 * (v.t / v.s);
             }
-            const bool none = v.s == 0.f;  // a row of -inf alone
-            const float ls = none ? INFINITY : logf(v.s), H = none ? 0.f : ls - kLn2 * (v.t / v.s);
             float g = 0.f, h = 0.f;
             if (lane == 0 && there) {
-                const float l = !counts ? 0.f : token >= V ? NAN : none ? -INFINITY : logp_of(to_f(x[token]), v.m, ls, q.scale, c);
+                const float l = !counts ? 0.f : token >= V ? NAN : none ? -INFINITY : as_differences ? q.scale * (to_f(x[token]) - v.m) - ls : logp_of(to_f(x[token]), v.m, ls, q.scale, c);
                 if (A.logp) A.logp[r] = l;
                 if (A.entropy) A.entropy[r] = counts ? H : 0.f;
                 if (MODE == FORWARD && A.norm) {
@@ -369,10 +398,10 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                 const int src = (threadIdx.x & 31) / G * G;
                 g = __shfl_sync(0xFFFFFFFFu, g, src);
                 h = __shfl_sync(0xFFFFFFFFu, h, src);
-                gr.set(v.m, ls, g, h, H, q.scale, c, token, V);
+                gr.set(v.m, ls, g, h, H, q.scale, c, token, V, as_differences);
             }
         } else if (counts) {
-            gr.set(A.norm_in[2 * r], A.norm_in[2 * r + 1], A.dlogp[r], A.dentropy ? A.dentropy[r] : 0.f, A.dentropy ? A.entropy_in[r] : 0.f, q.scale, c, token, V);
+            gr.set(A.norm_in[2 * r], A.norm_in[2 * r + 1], A.dlogp[r], A.dentropy ? A.dentropy[r] : 0.f, A.dentropy ? A.entropy_in[r] : 0.f, q.scale, c, token, V, as_differences);
         }
         if (MODE != FORWARD && there) {
             if (!in_loss) gr.kind = 2;
