@@ -352,6 +352,7 @@ int anakin_noalloc_status(void* cuda_stream, int* device_status);
  * tokens are given), mask[r] != 0 (where a mask is given) and, for the losses, it belongs to a sequence.  What a row that does not count holds is
  * never used, NaN included: its outputs are zeros.  A token >= vocab gives NaN.  Logits of -inf are tokens without probability; a row of
  * nothing else has logp -inf, entropy 0 and a gradient of zeros.  NaN or +inf among a row's logits gives NaN.
+ * A row that some blocks share waits for their sums, with a limit: should one run out, what follows is NaN.
  * Offsets that do not ascend, or pass [0, rows], are an error of the caller's that the kernels answer with wrong numbers, within bounds.
  */
 enum { ANAKIN_DTYPE_F32 = 0, ANAKIN_DTYPE_BF16 = 1, ANAKIN_DTYPE_F16 = 2 };
@@ -370,7 +371,7 @@ typedef struct anakin_token_rows {
     int64_t sequences;     /* >= 0, < 2^31 */
     int32_t token_bytes;   /* 4 or 8: int32 or int64 */
     int32_t offset_bytes;  /* 4 or 8 */
-    float scale;           /* the distribution is softmax(scale * logits): one over the sampling temperature; > 0 */
+    float scale;           /* the distribution is softmax(scale * logits): one over the sampling temperature; > 0, at most 2^40 */
     uint32_t reserved;     /* 0 */
 } anakin_token_rows;
 

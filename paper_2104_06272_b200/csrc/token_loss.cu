@@ -22,7 +22,7 @@ int check_rows(const anakin_token_rows* p, bool need_logits, bool need_tokens, b
     if (need_offsets && !p->offsets) return ANAKIN_E_INVALID_ARG;
     if (need_logits) {
         if (p->dtype < ANAKIN_DTYPE_F32 || p->dtype > ANAKIN_DTYPE_F16) return ANAKIN_E_INVALID_ARG;
-        if (p->vocab < 1 || p->vocab >= LIMIT || p->ld < p->vocab || !(p->scale > 0.f) || !(p->scale < INFINITY)) return ANAKIN_E_INVALID_ARG;
+        if (p->vocab < 1 || p->vocab >= LIMIT || p->ld < p->vocab || !(p->scale > 0.f) || !(p->scale <= 1.0995116e12f)) return ANAKIN_E_INVALID_ARG;
         if (p->rows > 0 && (!p->logits || ((uintptr_t)p->logits & (p->dtype == ANAKIN_DTYPE_F32 ? 3 : 1)))) return ANAKIN_E_INVALID_ARG;
     }
     if (need_tokens && p->rows > 0 && !p->tokens) return ANAKIN_E_INVALID_ARG;

@@ -4,7 +4,7 @@
 // With x the logits of a row, c = scale log2(e), m = max x, M = c m rounded, d_j = c x_j - M (one fused multiply-add):
 //   s = sum 2^d,  t = sum 2^d d   in one pass, rescaled whenever m grows;   log p_j = ln2 d_j - ln s;   H = ln s - ln2 t / s
 //   dx_j = scale ( g ([j = token] - p_j) - h p_j (log p_j + H) ) = 2^d_j ( a + b d_j ) + [j = token] scale g
-// M's rounding is the same in every term and cancels.  Where m is beyond 2^100 (a row of nothing but masks of the type's lowest value), c x would
+// M's rounding is the same in every term and cancels.  Where m is beyond 2^80 (a row of nothing but masks of the type's lowest value), c x would
 // overflow: there d_j = c (x_j - m).  Terms that are -inf give 2^d = 0, and 0 times d is kept from being NaN by a lower bound on d, in those
 // groups of logits only that hold such a term.
 //
@@ -77,7 +77,7 @@ template <class T, int U> __device__ __forceinline__ void extremes(const uint4 (
     }
 }
 
-constexpr float kHuge = 1.2676506e30f;  // 2^100
+constexpr float kHuge = 1.2089258e24f;  // 2^80: times c (scale is at most 2^40) far from fp32's largest
 __device__ __forceinline__ bool usual(float m) { return fabsf(m) < kHuge; }
 
 // The factor, and its logarithm to base 2, from sums relative to m to sums relative to a larger maximum.
@@ -190,7 +190,7 @@ struct Acc {
 // What the gradient of a row needs: 2^d ( a + b d ), d = c x - off or c (x - off), and `onehot` more at the token.
 struct RowGrad {
     float off, a, b, onehot;
-    int token, kind;  // kind: 0 usual, 1 = from differences (m beyond 2^100, or a short row), 2 = zeros, 3 = NaN
+    int token, kind;  // kind: 0 usual, 1 = from differences (m beyond 2^80, or a short row), 2 = zeros, 3 = NaN
     __device__ __forceinline__ void set(float m, float ln_s, float g, float h, float H, float scale, float c, long long tok, long long V, bool as_differences = false) {
         const float ls2 = ln_s * kLog2e, inv = ex2(-ls2);
         const float a0 = -scale * (g + h * H), b0 = -scale * h * kLn2;  // p ( a0 + b0 log2 p ),  p = 2^d / s

@@ -115,6 +115,25 @@ def test_ties_and_specials(tk):
     assert y[2].isnan().all() and y[3, 3] == math.inf and y[3, 4] == 0
 
 
+def test_every_nan_is_one_code(tk):
+    """Whatever its sign: ReLU's gradient by sign bits must not lose it."""
+    for dt in DT.values():
+        x = torch.zeros(2, 32, dtype=dt, device="cuda")
+        x[0, 5], x[1, 6] = math.nan, -math.nan
+        x[1, 6] = torch.copysign(torch.tensor(math.nan), torch.tensor(-1.0)).to(dt)
+        _, ck = tk.ckpt_forward(x, "identity")
+        assert ck.codes[0, 5] == 0x7F and ck.codes[1, 6] == 0x7F and (ck.codes != 0).sum() == 2
+        assert tk.ckpt_weight_grad(ck, torch.ones(2, 3, device="cuda"), "relu")[[5, 6]].isnan().all()
+        dx = tk.ckpt_backward(ck, torch.ones_like(x), "relu")
+        assert dx[0, 5].isnan() and dx[1, 6].isnan() and dx.isnan().sum() == 2
+
+
+def test_no_rows(tk):
+    x = torch.empty(0, 40, device="cuda")
+    y, ck = tk.ckpt_forward(x, "silu")
+    assert y.shape == (0, 40) and tk.ckpt_unpack(ck).shape == (0, 40) and tk.ckpt_backward(ck, x, "silu").shape == (0, 40)
+
+
 def wgrad_want(ck, dy, act, tk):
     x = tk.ckpt_unpack(ck, torch.float32).double()
     return plain.act(act, x).t() @ dy.double(), plain.act(act, x).abs().t() @ dy.double().abs()

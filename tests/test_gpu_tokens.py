@@ -283,6 +283,60 @@ def test_policy_grad_is_the_three_calls(tk, R, V, pad, dtype, mean, kl):
         assert torch.equal(y, got.dlogits) and torch.equal(z.stats, got.stats)
 
 
+@pytest.mark.parametrize("scale", [1e-3, 40.0, 1e4, 2.0 ** 40])
+@pytest.mark.parametrize("V", [3, 200, 6000])
+def test_temperatures(tk, V, scale):
+    """Logits whose scaled differences are of ordinary size, shifted by thousands of them."""
+    x, tokens, g = make(8, V, torch.float32, V)
+    x /= scale
+    x[4:] += 16.0 / scale
+    l, H, _, _ = plain.logp(x, tokens, scale)
+    o = tk.logp(x, tokens, scale=scale)
+    near(o.logp, l, tol_logp(V, l) + 2.0 ** -22 * 40)  # (the exponent's products are of size 40)
+    near(o.entropy, H, rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
+
+
+def test_no_rows(tk):
+    x = torch.empty(0, 50, device="cuda")
+    t, e = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda")
+    o = tk.logp(x, t)
+    assert o.logp.numel() == 0 and tk.logp_backward(x, t, o.norm, e).shape == (0, 50)
+    f, obj = objective(tk)
+    p = tk.policy_grad(obj, x, t, e, e, ref_logp=e)
+    assert (p.stats == 0).all() and p.dlogits.shape == (0, 50)
+    assert tk.logp(logits=torch.zeros(2, 4, device="cuda"), tokens=torch.zeros(2, dtype=torch.int64, device="cuda")).logp.shape == (2,)
+
+
+def test_a_first_call_may_be_a_captured_one(tk, tmp_path):
+    """In a process of its own, where no kernel of these has run."""
+    import subprocess
+    import sys
+
+    code = """
+import torch
+from paper_2104_06272_b200 import tokens as tk
+x = torch.randn(40, 30000, device="cuda", dtype=torch.bfloat16)
+t = torch.randint(0, 30000, (40,), device="cuda")
+a = torch.randn(40, device="cuda")
+h = torch.randn(300, 200, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    o = tk.policy_grad(tk.policy_objective(), x, t, None, a)
+    y, ck = tk.ckpt_forward(h)
+    w = tk.ckpt_weight_grad(ck, h, "relu")
+g.replay()
+torch.cuda.synchronize()
+p = tk.policy_grad(tk.policy_objective(), x, t, None, a)
+assert torch.equal(o.dlogits, p.dlogits) and torch.equal(w, tk.ckpt_weight_grad(ck, h, "relu"))
+"""
+    import os
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
 def test_columns_behind_the_vocabulary_stay(tk):
     x, tokens, g = make(20, 5001, torch.bfloat16, 1)
     out = torch.full((20, 5016), 7.0, dtype=torch.bfloat16, device="cuda")
