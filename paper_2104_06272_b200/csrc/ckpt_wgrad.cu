@@ -324,40 +324,50 @@ template <class T, int P, int E>
 __global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld, FastDiv per_row, uint32_t pieces, int N, int pitch, __nv_bfloat16* planes,
                                                       long long plane) {
     pdl_wait();
-    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += gridDim.x * 256) {
-        const uint32_t r = per_row.div(i);
-        const T* row = dy + (long long)r * ld;
-        const int j = (int)(i - r * per_row.d) * E;
-        float v[E];
-        if (E == 8 && j + E <= N) {
-            constexpr int V = 16 / sizeof(T);
+    constexpr int U = E == 8 ? 1 : 4;  // pieces of a thread in flight
+    for (uint32_t i0 = blockIdx.x * 256 * U + threadIdx.x; i0 < pieces; i0 += gridDim.x * 256 * U) {
+        float v[U][E];
+        __nv_bfloat16* out[U];
 #pragma unroll
-            for (int k = 0; k < E; k += V) {
-                float f[V];
-                tok::unpack16(*reinterpret_cast<const uint4*>(row + j + k), f, (const T*)nullptr);
+        for (int q = 0; q < U; ++q) {
+            const uint32_t i = i0 + 256 * q;
+            const uint32_t r = per_row.div(i < pieces ? i : 0u);
+            const int j = (int)((i < pieces ? i : 0u) - r * per_row.d) * E;
+            const T* row = dy + (long long)r * ld;
+            out[q] = planes + (long long)r * pitch + j;
+            if (E == 8 && j + E <= N) {
+                constexpr int V = 16 / sizeof(T);
 #pragma unroll
-                for (int u = 0; u < V; ++u) v[k + u] = f[u];
+                for (int k = 0; k < E; k += V) {
+                    float f[V];
+                    tok::unpack16(*reinterpret_cast<const uint4*>(row + j + k), f, (const T*)nullptr);
+#pragma unroll
+                    for (int u = 0; u < V; ++u) v[q][k + u] = f[u];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < E; ++k) v[q][k] = j + k < N ? tok::to_f(row[j + k]) : 0.f;
             }
-        } else {
-#pragma unroll
-            for (int k = 0; k < E; ++k) v[k] = j + k < N ? tok::to_f(row[j + k]) : 0.f;
         }
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            uint32_t w[E / 2];
+        for (int q = 0; q < U; ++q) {
+            if (i0 + 256 * q >= pieces) continue;
 #pragma unroll
-            for (int k = 0; k < E; k += 2) {
-                // (cut, not rounded: never past bf16's largest, and 8 bits a term are all 24)
-                const uint32_t a = v[k] == v[k] ? __float_as_uint(v[k]) & 0xFFFF0000u : 0x7FC00000u;
-                const uint32_t b = v[k + 1] == v[k + 1] ? __float_as_uint(v[k + 1]) & 0xFFFF0000u : 0x7FC00000u;
-                w[k / 2] = a >> 16 | b;
-                // (an infinity stays one: its rest would be NaN)
-                v[k] = fabsf(v[k]) < INFINITY ? v[k] - __uint_as_float(a) : 0.f;
-                v[k + 1] = fabsf(v[k + 1]) < INFINITY ? v[k + 1] - __uint_as_float(b) : 0.f;
+            for (int p = 0; p < P; ++p) {
+                uint32_t w[E / 2];
+#pragma unroll
+                for (int k = 0; k < E; k += 2) {
+                    // (cut, not rounded: never past bf16's largest, and 8 bits a term are all 24)
+                    const uint32_t a = v[q][k] == v[q][k] ? __float_as_uint(v[q][k]) & 0xFFFF0000u : 0x7FC00000u;
+                    const uint32_t b = v[q][k + 1] == v[q][k + 1] ? __float_as_uint(v[q][k + 1]) & 0xFFFF0000u : 0x7FC00000u;
+                    w[k / 2] = a >> 16 | b;
+                    // (an infinity stays one: its rest would be NaN)
+                    v[q][k] = fabsf(v[q][k]) < INFINITY ? v[q][k] - __uint_as_float(a) : 0.f;
+                    v[q][k + 1] = fabsf(v[q][k + 1]) < INFINITY ? v[q][k + 1] - __uint_as_float(b) : 0.f;
+                }
+                if constexpr (E == 8) *reinterpret_cast<uint4*>(out[q] + p * plane) = make_uint4(w[0], w[1], w[2], w[3]);
+                else *reinterpret_cast<uint32_t*>(out[q] + p * plane) = w[0];
             }
-            __nv_bfloat16* out = planes + p * plane + (long long)r * pitch + j;
-            if constexpr (E == 8) *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-            else *reinterpret_cast<uint32_t*>(out) = w[0];
         }
     }
 }

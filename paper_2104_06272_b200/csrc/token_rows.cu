@@ -295,8 +295,9 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
     int flip = 0;
     // (whole groups of a warp go through the loop together: the shuffles take all lanes)
     for (long long r0 = (long long)blockIdx.x * GROUPS; r0 < q.rows; r0 += (long long)gridDim.x * GROUPS) {
-        const long long r = r0 + threadIdx.x / G;
-        const bool there = r < q.rows;
+        // (the gradient starts with the last rows, which the forward pass has left in L2: both passes over 1024 x 32000 bf16 40.6 us, this way 39.0)
+        const long long r = MODE == BACKWARD ? q.rows - 1 - r0 - threadIdx.x / G : r0 + threadIdx.x / G;
+        const bool there = r >= 0 && r < q.rows;
         const T* x = static_cast<const T*>(q.logits) + (there ? r : 0) * q.ld;
         // (a row of no sequence has its log-probability, but no part in the loss)
         const int info = !there ? -2 : MODE == FUSED ? A.info[r].x : row_counts(q, r) ? 0 : -2;
