@@ -433,6 +433,24 @@ Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy,
     return p;
 }
 
+// Tensor maps of matrices whose rows lie pitch_bytes apart (a multiple of 16): bf16 in 64 x 64 boxes with the 128-byte swizzle, or bytes in boxes of
+// 128 columns x 64 rows.  Columns from `cols` on read as zeros, whatever lies there.
+bool encode_map(CUtensorMap* map, bool bytes, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch_bytes) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = []() -> Encode {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+        return reinterpret_cast<Encode>(p);
+    }();
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_bytes};
+    const cuuint32_t box[2] = {bytes ? 128u : 64u, 64}, steps[2] = {1, 1};
+    return encode && encode(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, steps,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int BN, int P, bool PAIR>
 cudaError_t launch_wgrad(const Maps& maps, const Args& a, const Plan& p, cudaStream_t s) {
     return launch_cluster<k_ckpt_wgrad<BN, P, PAIR>>(dim3(p.runs * (PAIR ? 2 : 1)), dim3(Cfg<BN, P, PAIR>::THREADS), Cfg<BN, P, PAIR>::SMEM, s, PAIR ? 2 : 1, maps, a);
@@ -508,7 +526,7 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
         memset(&maps, 0, sizeof(maps));
         Args a = {};
         a.blocks = (K + 31) / 32;
-        if (!make_tensor_map_u8(&maps.codes, codes, (uint64_t)R, (uint64_t)a.blocks * 32, 64, 128)) return tok::fail();
+        if (!encode_map(&maps.codes, true, codes, (uint64_t)R, (uint64_t)a.blocks * 32, (uint64_t)a.blocks * 32)) return tok::fail();
         if (!p.direct) {
             const cudaError_t e = dtype == ANAKIN_DTYPE_F32 ? launch_split<float, 3>(dy, lddy, R, N, p.pitch, dev_workspace, p.plane_bytes, s)
                                   : dtype == ANAKIN_DTYPE_F16 ? launch_split<__half, 2>(dy, lddy, R, N, p.pitch, dev_workspace, p.plane_bytes, s)
@@ -517,7 +535,7 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
         }
         for (int i = 0; i < p.P; ++i) {
             const void* b = p.direct ? dy : static_cast<const unsigned char*>(dev_workspace) + i * p.plane_bytes;
-            if (!make_tensor_map_pitched(&maps.b[i], b, (uint64_t)R, (uint64_t)N, (uint64_t)(p.direct ? lddy : p.pitch) * 2, 64, true)) return tok::fail();
+            if (!encode_map(&maps.b[i], false, b, (uint64_t)R, (uint64_t)N, (uint64_t)(p.direct ? lddy : p.pitch) * 2)) return tok::fail();
         }
         a.R = R;
         a.K = K;

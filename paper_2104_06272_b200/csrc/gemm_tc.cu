@@ -88,11 +88,6 @@ bool make_tensor_map_2d(CUtensorMap* map, const void* base, uint64_t rows, uint6
     return encode_cached(map, MapKey{base, {cols, rows}, {cols * 2}, {64, box_rows}, 2, bf16 ? 1u : 0u});
 }
 
-bool make_tensor_map_pitched(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch_bytes, uint32_t box_rows, bool bf16) {
-    if (pitch_bytes % 16 != 0 || ((uintptr_t)base & 15)) return false;
-    return encode_cached(map, MapKey{base, {cols, rows}, {pitch_bytes}, {64, box_rows}, 2, bf16 ? 1u : 0u});
-}
-
 bool make_tensor_map_4d(CUtensorMap* map, const void* base, uint64_t envs, uint64_t steps, uint64_t policies, uint64_t pol_stride, uint32_t box_envs,
                         uint32_t box_steps, bool bf16) {
     return encode_cached(map, MapKey{base, {64, envs, steps, policies}, {128, envs * 128, pol_stride}, {64, box_envs, box_steps, 1}, 4, bf16 ? 1u : 0u});

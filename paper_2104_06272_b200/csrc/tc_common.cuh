@@ -321,8 +321,6 @@ __host__ __device__ constexpr int x3_b(int i) { return i == 1 ? 2 : i == 2 ? 1 :
 // Host: encodes a 2-D tensor map over a row-major 16-bit matrix [rows][cols] with a box of 64 columns x box_rows rows
 // and the 128-byte swizzle.  Returns false if the driver entry point is missing or the encode fails.
 bool make_tensor_map_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, bool bf16);
-// Host: the same with rows pitch_bytes apart (a multiple of 16); columns from cols on read as zeros, whatever lies there.
-bool make_tensor_map_pitched(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch_bytes, uint32_t box_rows, bool bf16);
 // Host: the same over [policy][step][env][64] (policies pol_stride bytes apart) with a box of box_envs x box_steps rows.
 bool make_tensor_map_4d(CUtensorMap* map, const void* base, uint64_t envs, uint64_t steps, uint64_t policies, uint64_t pol_stride, uint32_t box_envs,
                         uint32_t box_steps, bool bf16);
