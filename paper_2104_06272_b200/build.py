@@ -1,4 +1,4 @@
-"""Builds libanakin.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Builds libanakin.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _tokens_host.so (the Python module behind tokens.py) with g++.
 
 Each .cu file is compiled to an object of its own (in parallel, only when it or a header changed) under
 `_build/`, then the objects are linked into the shared library.  No relocatable device code is used: every
@@ -7,9 +7,11 @@ translation unit carries its own kernels.
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -17,7 +19,10 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libanakin.so")
+HOST_SRC = os.path.join(CSRC, "tokens_host.cpp")
+HOST = os.path.join(HERE, "_tokens_host.so")
 
+NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -48,10 +53,32 @@ def stale() -> bool:
     return any(os.path.getmtime(p) > t for p in sources() + headers())
 
 
+def host_stale() -> bool:
+    header = os.path.join(ROOT, "include", "anakin.h")
+    return not os.path.exists(HOST) or any(os.path.getmtime(p) > os.path.getmtime(HOST) for p in (HOST_SRC, header))
+
+
+def build_host() -> None:
+    """The module links to torch's libraries and to libanakin.so beside it."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")
+    inc = [os.path.join(ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(torch, "include"),
+           os.path.join(torch, "include", "torch", "csrc", "api", "include"), cuda]
+    libs = ["-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", HERE, "-l:libanakin.so", "-Wl,-rpath,$ORIGIN"]
+    tmp = HOST + f".tmp{os.getpid()}"
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared"] + [a for i in inc for a in ("-isystem", i)] + ["-o", tmp, HOST_SRC] + libs)
+    os.replace(tmp, HOST)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not stale():
-        return LIB
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    if force or stale():
+        build_lib(force, verbose)
+    if force or host_stale():
+        build_host()
+    return LIB
+
+
+def build_lib(force: bool, verbose: bool) -> None:
     os.makedirs(OBJ, exist_ok=True)
     hdr_time = max(os.path.getmtime(p) for p in headers())
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -59,16 +86,15 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
     def compile_one(src: str) -> None:
         tmp = _obj(src) + f".tmp{os.getpid()}"
-        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + inc + ["-c", "-o", tmp, src]
+        cmd = [NVCC] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + inc + ["-c", "-o", tmp, src]
         subprocess.check_call(cmd)
         os.replace(tmp, _obj(src))
 
     with ThreadPoolExecutor(max_workers=min(len(todo), os.cpu_count() or 4) or 1) as ex:
         list(ex.map(compile_one, todo))
     tmp = LIB + f".tmp{os.getpid()}"
-    subprocess.check_call([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", tmp] + [_obj(s) for s in sources()])
+    subprocess.check_call([NVCC, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", tmp] + [_obj(s) for s in sources()])
     os.replace(tmp, LIB)
-    return LIB
 
 
 if __name__ == "__main__":
