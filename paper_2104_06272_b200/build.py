@@ -64,7 +64,7 @@ def build_host() -> None:
     cuda = os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")
     inc = [os.path.join(ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(torch, "include"),
            os.path.join(torch, "include", "torch", "csrc", "api", "include"), cuda]
-    libs = ["-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", HERE, "-l:libanakin.so", "-Wl,-rpath,$ORIGIN"]
+    libs = ["-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-L", HERE, "-l:libanakin.so", "-Wl,-rpath,$ORIGIN"]
     tmp = HOST + f".tmp{os.getpid()}"
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared"] + [a for i in inc for a in ("-isystem", i)] + ["-o", tmp, HOST_SRC] + libs)
     os.replace(tmp, HOST)

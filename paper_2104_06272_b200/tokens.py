@@ -1,10 +1,10 @@
 """Policies over token vocabularies, and activation checkpoints in 8 bits: Python functions over the stateless calls of include/anakin.h
 (anakin_token_*, anakin_ckpt_*), which say what each computes.
 
-Argument marshalling only, done in C++ (csrc/tokens_host.cpp): the smallest calls cost the host more than the GPU.  Tensors lie on one CUDA device; work is enqueued on that device's current torch stream, outputs and
-workspaces come from torch's allocator on that stream, nothing synchronises, and every call may be captured into a CUDA graph.  Gradients
-are outputs (`logits.backward(dlogits)` hands one to autograd); the inputs are not differentiated through.  What a call refuses it
-refuses with AnakinError before anything is enqueued.
+Argument marshalling only, done in C++ (csrc/tokens_host.cpp), as the smallest calls cost the host more than the GPU.  Tensors lie on one
+CUDA device; work is enqueued on that device's current torch stream, outputs and workspaces come from torch's allocator on that stream,
+nothing synchronises, and every call may be captured into a CUDA graph.  Gradients are outputs (`logits.backward(dlogits)` hands one to
+autograd); the inputs are not differentiated through.  What a call refuses it refuses with AnakinError before anything is enqueued.
 """
 from __future__ import annotations
 

@@ -262,3 +262,32 @@ def test_matrices_past_32_bits(tk):
     x.fill_(1.0)
     tk.ckpt_backward(ck, x, "relu", out=x)
     assert torch.equal(x[-1], (torch.arange(K, device="cuda") % 13 > 6).to(torch.bfloat16)) and (x[-2] == 0).all()
+
+
+def test_refusals_of_tensors(tk):
+    """Types, shapes, strides and devices that do not fit; nothing is enqueued and the next call is sound."""
+    x = torch.randn(6, 40, device="cuda")
+    y, ck = tk.ckpt_forward(x)
+    dy = torch.randn(6, 8, device="cuda")
+    q, s, _ = ck
+    Ck = tk.Checkpoint
+    bad = [Ck(q, s, 0), Ck(q, s, -3), Ck(q, s, 70), Ck(q, s, 32), Ck(q, s, 1 << 40), Ck(q[:, :40], s, 40), Ck(q.int(), s, 40), Ck(q.cpu(), s.cpu(), 40), Ck(q, s.cpu(), 40),
+           Ck(q, s[:5], 40), Ck(q, s.t().contiguous().t(), 40), Ck(q[:5], s, 40), Ck(None, s, 40), Ck(q, None, 40)]
+    calls = [lambda f=f, c=c: f(c) for c in bad for f in (tk.ckpt_unpack, lambda c: tk.ckpt_backward(c, x), lambda c: tk.ckpt_weight_grad(c, dy))]
+    calls += [lambda: tk.ckpt_forward(x.double()), lambda: tk.ckpt_forward(x.t()), lambda: tk.ckpt_forward(x, "tanh"), lambda: tk.ckpt_forward(x, out=x.half()),
+              lambda: tk.ckpt_forward(x, out=x[:5]), lambda: tk.ckpt_unpack(ck, torch.float64), lambda: tk.ckpt_unpack(ck, out=x.double()), lambda: tk.ckpt_unpack(ck, out=x[:, 1:]),
+              lambda: tk.ckpt_backward(ck, x[:5]), lambda: tk.ckpt_backward(ck, None), lambda: tk.ckpt_backward(ck, x.cpu()), lambda: tk.ckpt_backward(ck, x, "tanh"),
+              lambda: tk.ckpt_backward(ck, x, out=x.half()), lambda: tk.ckpt_weight_grad(ck, dy[:5]), lambda: tk.ckpt_weight_grad(ck, dy, accumulate=True),
+              lambda: tk.ckpt_weight_grad(ck, dy, out=torch.zeros(40, 8, device="cuda").half()), lambda: tk.ckpt_weight_grad(ck, dy, out=torch.zeros(8, 40, device="cuda")),
+              lambda: tk.ckpt_weight_grad(ck, dy, status=torch.zeros(1, device="cuda")), lambda: tk.ckpt_weight_grad(ck, dy, status=torch.zeros(2, dtype=torch.int32, device="cuda"))]
+    for i, call in enumerate(calls):
+        with pytest.raises(tk.AnakinError) as e:
+            call()
+            print(f"call {i} was taken")
+        assert e.value.code == -1, i
+    for act in ("silu", "gelu"):
+        with pytest.raises(tk.AnakinError) as e:
+            tk.ckpt_weight_grad(ck, dy, act)
+        assert e.value.code == -4
+    again = tk.ckpt_forward(x)
+    assert torch.equal(again[0], y) and torch.equal(again[1].codes, q) and torch.equal(again[1].scales, s)

@@ -491,3 +491,61 @@ def test_rows_past_32_bits(tk):
     tk.logp_backward(x, tokens, o.norm, d, out=x)
     want = plain.dlogits(torch.zeros(1, V, device="cuda"), tokens[:1], d[:1])
     near(x[-2:-1], want, 2.0 ** -8 * want.abs() + 1e-9)
+
+
+def test_refusals_of_tensors(tk):
+    """Types, shapes, strides and devices that do not fit; nothing is enqueued and the next call is sound."""
+    x, tokens, _ = make(6, 10, torch.float32)
+    v, w = torch.zeros(6, device="cuda"), torch.zeros(12, device="cuda")[::2]
+    obj, po, off = tk.policy_objective(), tk.preference_objective(), torch.tensor([0, 3, 6], device="cuda")
+    kl = tk.policy_objective(kl="k3", kl_coef=0.1)
+    want = tk.logp(x, tokens)
+    norm = want.norm
+    calls = [
+        lambda: tk.logp(None, tokens), lambda: tk.logp(x.double(), tokens), lambda: tk.logp(x.t(), tokens), lambda: tk.logp(x[:, :0], tokens), lambda: tk.logp(x[0], tokens),
+        lambda: tk.logp(x, None), lambda: tk.logp(x, tokens[:5]), lambda: tk.logp(x, tokens.cpu()), lambda: tk.logp(x, tokens.float()), lambda: tk.logp(x, tokens.view(2, 3)),
+        lambda: tk.logp(x, tokens, mask=v), lambda: tk.logp(x, tokens, 0.0), lambda: tk.logp(x, tokens, 1e300), lambda: tk.logp(x.expand(6, 10)[:1].expand(6, 10), tokens),
+        lambda: tk.logp_backward(x, tokens, norm, None), lambda: tk.logp_backward(x, tokens, norm[:5], v), lambda: tk.logp_backward(x, tokens, norm, w),
+        lambda: tk.logp_backward(x, tokens, norm, v, None, v), lambda: tk.logp_backward(x, tokens, norm, v, out=x.half()), lambda: tk.logp_backward(x, tokens, norm, v, out=x[:5]),
+        lambda: tk.logp_backward(x, tokens, torch.zeros(6, 4, device="cuda")[:, :2], v), lambda: tk.policy_loss(obj, x, v, v), lambda: tk.policy_loss(obj, v, v, None),
+        lambda: tk.policy_loss(kl, v, v, v), lambda: tk.policy_loss(po, v, v, v), lambda: tk.policy_loss(obj, v, v, v, offsets=off[:0]),
+        lambda: tk.policy_loss(obj, v, v, v, offsets=off.view(1, 3)), lambda: tk.policy_grad(obj, x, None, v, v), lambda: tk.policy_grad(kl, x, tokens, v, v),
+        lambda: tk.policy_grad(obj, x, tokens, v, v.half()), lambda: tk.preference_loss(obj, v, off), lambda: tk.preference_loss(po, v, None),
+        lambda: tk.preference_loss(po, v, off[:2]), lambda: tk.preference_loss(po, v.half(), off)]
+    for i, call in enumerate(calls):
+        with pytest.raises(tk.AnakinError) as e:
+            call()
+            print(f"call {i} was taken")
+        assert e.value.code == -1, i
+    for call in (lambda: tk.logp(x, tokens, "1"), lambda: tk.policy_loss(None, v, v, v)):
+        with pytest.raises(TypeError):
+            call()
+    again = tk.logp(x, tokens)
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+
+
+def test_two_threads_on_streams_of_their_own(tk):
+    """Calls from several host threads at once share nothing."""
+    import threading
+
+    x, tokens, g = make(700, 3000, torch.bfloat16, 5, ignored=0.2)
+    obj = tk.policy_objective(mean="sequence")
+    adv = torch.randn(700, generator=g, device="cuda")
+    offsets = torch.tensor([0, 400, 700], device="cuda")
+    want = tk.policy_grad(obj, x, tokens, None, adv, offsets=offsets)
+    torch.cuda.synchronize()
+    bad = []
+
+    def work():
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got = tk.policy_grad(obj, x, tokens, None, adv, offsets=offsets)
+                s.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(want, got)):
+                    bad.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(3)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not bad
