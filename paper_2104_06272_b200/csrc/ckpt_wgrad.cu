@@ -8,10 +8,10 @@
 // A CTA, or a pair of CTAs whose tensor cores work as one, owns tiles of dW (128 x BN, or 256 x BN with a half of either operand in each CTA) and walks
 // over rows in chunks of 64:
 //   warp 0       TMA: the 64 x 128 codes and the planes of dY (64 x 64 boxes, 128-byte swizzle) into a ring of stages
-//   warps 4-11   two warpgroups turn codes into bf16 in the swizzled layout, a chunk each in turn (a thread makes 16 bytes of 8 codes of a row; block
-//                scales are fetched ahead)
+//   then         three warpgroups (two with more than one plane) turn codes into bf16 in the swizzled layout, a chunk each in turn (a thread makes 16
+//                bytes of 8 codes of a row; block scales are fetched ahead)
 //   warp 1       (of a pair: the first CTA's) tcgen05.mma into one of two accumulators in tensor memory; commits free the stage
-//   warps 12-19  add a finished accumulator to sums in registers; behind a tile's last chunk store them
+//   and two      add a finished accumulator to sums in registers; behind a tile's last chunk store them
 // The tensor core's fp32 accumulation rounds toward zero, which biases long sums (about 5e-8 of the sum an MMA): an accumulator takes at most 32
 // MMAs (512 rows of one bf16 term) and the groups are added with round-to-nearest.
 // The chunks of all tiles, one tile after the other, are dealt out in equal runs, so that every SM has the same work; a tile that several runs share is
@@ -20,6 +20,7 @@
 // fetched and read once by each).  524288 x 1024 x 1024 bf16: 975 us, 1.13 PFLOP/s (cuBLAS, the bf16 product alone: 826).
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "ckpt.cuh"
 #include "tc_common.cuh"
@@ -51,9 +52,9 @@ struct Args {
     long long run, total;          // chunks of a run, of all tiles
     int per_tile, tiles;           // per_tile > 0: so many runs to each tile, all tiles' first ones first; 0: runs go on from one tile to the next
     const uint8_t* scales;
-    float* out;                    // dW, or partial tiles: that of a tile's i-th run at i * part_stride.  16-byte aligned, ld and width multiples of 4
+    float* out;                    // dW, or partial tiles: that of a tile's i-th run at i * part_stride
     long long ld, part_stride;
-    int width, relu;
+    int add, relu;                 // add: to what dW holds
     int32_t* status;
 };
 
@@ -77,6 +78,22 @@ struct Walk {
         left -= more;
     }
 };
+
+// v[J0 .. J0 + 31] of 32 lanes turned over: lane l's j-th becomes lane j's l-th.
+template <int J0, int COLS>
+__device__ __forceinline__ void transpose32(float (&v)[COLS], int lane) {
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (j & s) continue;
+            const bool up = lane & s;
+            const float x = __shfl_xor_sync(0xFFFFFFFFu, up ? v[J0 + j] : v[J0 + (j | s)], s);
+            if (up) v[J0 + j] = x;
+            else v[J0 + (j | s)] = x;
+        }
+    }
+}
 
 template <int BN, int P, bool PAIR>
 __global__ void __launch_bounds__((Cfg<BN, P, PAIR>::THREADS), 1) k_ckpt_wgrad(const __grid_constant__ Maps maps, Args a) {
@@ -280,11 +297,27 @@ __global__ void __launch_bounds__((Cfg<BN, P, PAIR>::THREADS), 1) k_ckpt_wgrad(c
 #pragma unroll
                     for (int j = 0; j < COLS; ++j) sum[j] = NAN;
                 }
-                float4* dst = reinterpret_cast<float4*>(a.out + (size_t)part * a.part_stride + (size_t)m * a.ld + nb);
-                const int width = m < a.K ? a.width - nb : 0;
+                // (a warp stores 32 neighbours of a row at a time; rows of dW may start anywhere)
+                float* row = a.out + (size_t)part * a.part_stride + (long long)(m - lane) * a.ld;
+                auto store = [&](auto first) {
+                    constexpr int J0 = decltype(first)::value;
+                    transpose32<J0>(sum, lane);
+                    const int n = nb + J0 + lane, rows = n < a.N ? min(a.K - (m - lane), 32) : 0;
+                    if (a.add) {
 #pragma unroll
-                for (int j = 0; j < COLS; j += 4)
-                    if (j < width) dst[j / 4] = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+                        for (int j = 0; j < 32; ++j)
+                            if (j < rows) sum[J0 + j] += row[j * a.ld + n];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < rows) row[j * a.ld + n] = sum[J0 + j];
+                };
+                store(std::integral_constant<int, 0>{});
+                if constexpr (COLS > 32) store(std::integral_constant<int, 32>{});
+                if constexpr (COLS > 64) {
+                    store(std::integral_constant<int, 64>{});
+                    store(std::integral_constant<int, 96>{});
+                }
 #pragma unroll
                 for (int j = 0; j < COLS; ++j) sum[j] = 0.f;
             }
@@ -300,53 +333,114 @@ __global__ void __launch_bounds__((Cfg<BN, P, PAIR>::THREADS), 1) k_ckpt_wgrad(c
     }
 }
 
-// Partial tiles summed in the order of the runs that left them; tile_k x tile_n each.
-__global__ void __launch_bounds__(256) k_wgrad_sum(const float* part, long long part_stride, int pitch, long long run, int per_tile, int chunks, int tiles_m, int tile_k, int tile_n, int K, int N,
-                                                   float* dw, long long ld, int add) {
+// Partial tiles summed in a fixed order.  WARPS = 1: a warp takes four segments of 32 neighbours of a row, a few parts each;
+// 8: a block takes one segment, every warp each 8th part of it, so that many parts of a small dW are all in flight.
+struct Parts {
+    const float* at;
+    long long stride;
+    FastDiv run;
+    int per_tile, chunks, tiles_m, log_k, log_n, pitch;  // (as in Args; a tile is 2^log_k x 2^log_n)
+    __device__ __forceinline__ int count(int k, int n) const {
+        if (per_tile > 0 || chunks == 0) return per_tile;
+        const uint32_t t = (uint32_t)((n >> log_n) * tiles_m + (k >> log_k)) * (uint32_t)chunks;
+        return (int)(run.div(t + chunks - 1) - run.div(t)) + 1;
+    }
+};
+template <int WARPS>
+__global__ void __launch_bounds__(256) k_wgrad_sum(Parts p, FastDiv per_row, uint32_t segments, int N, float* dw, long long ld, int add) {
     pdl_wait();
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)K * N; i += (long long)gridDim.x * 256) {
-        const int k = (int)(i / N), n = (int)(i - (long long)k * N);
-        int parts = 0;
-        if (chunks > 0) {
-            const long long t = (long long)(n / tile_n) * tiles_m + k / tile_k;
-            parts = per_tile > 0 ? per_tile : (int)((t * chunks + chunks - 1) / run - t * chunks / run) + 1;
+    constexpr int U = WARPS == 1 ? 4 : 1;
+    __shared__ float sums[8][33];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const uint32_t first = WARPS == 1 ? (blockIdx.x * 8 + wid) * U : blockIdx.x, step = gridDim.x * (WARPS == 1 ? 8 * U : 1);
+    for (uint32_t i0 = first; i0 < segments; i0 += step) {
+        float v[U], old[U];
+        const float* src[U];
+        float* dst[U];
+        int parts[U], most = 0;
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const uint32_t i = min(i0 + q, segments - 1), k = per_row.div(i);
+            const int n = (int)(i - k * per_row.d) * 32 + lane;
+            parts[q] = i0 + q < segments && n < N ? p.count((int)k, n) : 0;
+            src[q] = p.at + (size_t)k * p.pitch + n;
+            dst[q] = i0 + q < segments && n < N ? dw + k * ld + n : nullptr;
+            old[q] = add && dst[q] && wid % WARPS == 0 ? *dst[q] : 0.f;
+            v[q] = 0.f;
+            most = max(most, parts[q]);
         }
-        float v = 0.f;
-        for (int s = 0; s < parts; ++s) v += part[(size_t)s * part_stride + (size_t)k * pitch + n];
-        float* p = dw + k * ld + n;
-        *p = add ? *p + v : v;
+        if constexpr (WARPS == 1) {
+            for (int s = 0; s < most; ++s) {
+#pragma unroll
+                for (int q = 0; q < U; ++q)
+                    if (s < parts[q]) v[q] += src[q][(size_t)s * p.stride];
+            }
+        } else {
+#pragma unroll 8
+            for (int s = wid; s < most; s += 8) v[0] += src[0][(size_t)s * p.stride];
+            sums[wid][lane] = v[0];
+            __syncthreads();
+            v[0] = 0.f;
+            if (wid == 0) {
+#pragma unroll
+                for (int w = 0; w < 8; ++w) v[0] += sums[w][lane];
+            }
+            __syncthreads();
+            if (wid != 0) continue;
+        }
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+            if (dst[q]) *dst[q] = add ? old[q] + v[q] : v[q];
     }
 }
 
 // dY as P bf16 planes [rows][pitch] that sum to it (fp32: 24 bits in three; fp16: 11 bits in two; bf16 whose rows TMA cannot address: one).  A thread
-// takes E neighbouring elements: 8 where rows start on 16-byte boundaries, else 2, so that a warp's loads lie side by side.
-template <class T, int P, int E>
+// takes 8 neighbouring elements: as 16-byte words where rows start on such boundaries (VEC), else as 4-byte words, those of 16-bit types that start
+// in the middle of one shifted into place (5003 x 4099 bf16: 15 us, by 2-byte loads 19.5).
+template <class T, int P, bool VEC>
 __global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld, FastDiv per_row, uint32_t pieces, int N, int pitch, __nv_bfloat16* planes,
                                                       long long plane) {
     pdl_wait();
-    constexpr int U = E == 8 ? 1 : 4;  // pieces of a thread in flight
+    constexpr int E = 8, U = VEC ? 1 : 2;  // U: pieces of a thread in flight
     for (uint32_t i0 = blockIdx.x * 256 * U + threadIdx.x; i0 < pieces; i0 += gridDim.x * 256 * U) {
         float v[U][E];
         __nv_bfloat16* out[U];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-            const uint32_t i = i0 + 256 * q;
-            const uint32_t r = per_row.div(i < pieces ? i : 0u);
-            const int j = (int)((i < pieces ? i : 0u) - r * per_row.d) * E;
-            const T* row = dy + (long long)r * ld;
+            const uint32_t i = min(i0 + 256 * q, pieces - 1);
+            const uint32_t r = per_row.div(i);
+            const int j = (int)(i - r * per_row.d) * E;
+            const T* src = dy + (long long)r * ld + j;
+            const int odd = sizeof(T) == 2 ? (int)((uintptr_t)src >> 1 & 1) : 0;  // from the middle of a word on
             out[q] = planes + (long long)r * pitch + j;
-            if (E == 8 && j + E <= N) {
+            if (j >= odd && j + E + odd <= N) {  // (whole words lie within the row)
+                constexpr int W = E * (int)sizeof(T) / 4;
+                uint32_t w[W + 1];
+                if constexpr (VEC) {
+#pragma unroll
+                    for (int k = 0; k < W; k += 4) *reinterpret_cast<uint4*>(w + k) = reinterpret_cast<const uint4*>(src)[k / 4];
+                } else {
+                    const uint32_t* at = reinterpret_cast<const uint32_t*>(src - odd);
+#pragma unroll
+                    for (int k = 0; k < W; ++k) w[k] = at[k];
+                    if (odd) {
+                        w[W] = at[W];
+#pragma unroll
+                        for (int k = 0; k < W; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+                    }
+                }
                 constexpr int V = 16 / sizeof(T);
 #pragma unroll
                 for (int k = 0; k < E; k += V) {
                     float f[V];
-                    tok::unpack16(*reinterpret_cast<const uint4*>(row + j + k), f, (const T*)nullptr);
+                    const int k4 = k * (int)sizeof(T) / 4;
+                    tok::unpack16(make_uint4(w[k4], w[k4 + 1], w[k4 + 2], w[k4 + 3]), f, (const T*)nullptr);
 #pragma unroll
                     for (int u = 0; u < V; ++u) v[q][k + u] = f[u];
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < E; ++k) v[q][k] = j + k < N ? tok::to_f(row[j + k]) : 0.f;
+                for (int k = 0; k < E; ++k) v[q][k] = j + k < N ? tok::to_f(src[k]) : 0.f;
             }
         }
 #pragma unroll
@@ -365,8 +459,7 @@ __global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld,
                     v[q][k] = fabsf(v[q][k]) < INFINITY ? v[q][k] - __uint_as_float(a) : 0.f;
                     v[q][k + 1] = fabsf(v[q][k + 1]) < INFINITY ? v[q][k + 1] - __uint_as_float(b) : 0.f;
                 }
-                if constexpr (E == 8) *reinterpret_cast<uint4*>(out[q] + p * plane) = make_uint4(w[0], w[1], w[2], w[3]);
-                else *reinterpret_cast<uint32_t*>(out[q] + p * plane) = w[0];
+                *reinterpret_cast<uint4*>(out[q] + p * plane) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
     }
@@ -379,7 +472,7 @@ struct Plan {
     size_t plane_bytes, part_off, bytes;
 };
 
-Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy, long long lddy, const void* dw, long long lddw, bool add) {
+Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy, long long lddy) {
     Plan p = {};
     p.P = dtype == ANAKIN_DTYPE_F32 ? 3 : dtype == ANAKIN_DTYPE_F16 ? 2 : 1;
     p.pair = K > 128 && N > 64;  // (a pair's second CTA has the second 128 rows of dW)
@@ -395,11 +488,11 @@ Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy,
     p.total = tiles * p.chunks;
     // Either every tile gets the same number of runs: then all tiles' runs of the same rows are at work at one time and what they read comes from L2.
     // Or runs of the same length go on from tile to tile and every SM is busy; then, where codes and dY are more than L2 holds, each tile reads its
-    // own from memory.  A run has four chunks at least; a chunk takes some 0.4 us (one term; 0.3 a term with more), a MB of partial sums written and
-    // read 0.25 us, a kernel or another wave of runs 2.
-    p.width = (int)((N + 3) / 4 * 4);
+    // own from memory.  A run has four chunks at least; a chunk takes some 0.47 us (one term; 0.3 a term with more), a MB of partial sums written
+    // and read 0.5 us, a kernel or another wave of runs 2.
+    p.width = (int)((N + 31) / 32 * 32);
     if (p.chunks == 0) return p;
-    const double us = p.P == 1 ? 0.4 : 0.3 * p.P, part_us = 1e-6 * (double)K * (double)N;
+    const double us = p.P == 1 ? 0.47 : 0.3 * p.P, part_us = 2e-6 * (double)K * (double)N;
     const double tiles_n = (double)((N + p.BN - 1) / p.BN), code_mb = 1e-6 * R * K, dy_mb = 2e-6 * R * N * p.P;
     const long long most_each = std::max(1ll, std::min((p.chunks + 3ll) / 4, 3ll * most / tiles));
     long long even = p.chunks;
@@ -417,7 +510,7 @@ Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy,
     if (flow < 4) flow = 4;
     const double read = (code_mb + dy_mb > 100.0 ? code_mb * tiles_n + dy_mb * p.tiles_m : code_mb + dy_mb) / 5.5;
     const double t_flow = std::max(us * (double)flow, read) + 4.0 + part_us * 3.0;
-    if (t_even <= t_flow) {
+    if (t_even <= t_flow || p.total >= (1ll << 31)) {  // (k_wgrad_sum counts the chunks of flowing runs in 32 bits)
         p.per_tile = (int)each;
         p.run = even;
         p.parts = p.per_tile;
@@ -425,10 +518,10 @@ Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy,
     } else {
         p.run = flow;
         p.parts = (int)((p.chunks + p.run - 2) / p.run) + 1;
-        p.runs = p.run < (1ll << 30) ? (int)((p.total + p.run - 1) / p.run) : 0;
+        p.runs = (int)((p.total + p.run - 1) / p.run);
     }
     p.part_off = p.direct ? 0 : (size_t)p.P * p.plane_bytes;
-    p.straight = R > 0 && p.parts == 1 && !add && ((uintptr_t)dw & 15) == 0 && lddw % 4 == 0 && N % 4 == 0;
+    p.straight = p.parts == 1;
     p.bytes = p.part_off + (p.straight ? 0 : (size_t)p.parts * K * p.width * 4);
     return p;
 }
@@ -467,15 +560,15 @@ cudaError_t launch_wgrad_p(const Maps& maps, const Args& a, const Plan& p, cudaS
 template <class T, int P>
 cudaError_t launch_split(const void* dy, long long ld, int R, int N, int pitch, void* ws, size_t plane_bytes, cudaStream_t s) {
     const bool vec = ((uintptr_t)dy & 15) == 0 && ld * sizeof(T) % 16 == 0;
-    const int per_row = pitch / (vec ? 8 : 2);
+    const int per_row = pitch / 8;
     const long long most = ((1ll << 31) - 1) / per_row;  // rows of a launch: fewer than 2^31 pieces
     for (long long r0 = 0; r0 < R; r0 += most) {
         const uint32_t pieces = (uint32_t)(std::min(most, R - r0) * per_row), ctas = (pieces + 255) / 256;
         const T* from = static_cast<const T*>(dy) + r0 * ld;
         __nv_bfloat16* planes = static_cast<__nv_bfloat16*>(ws) + r0 * pitch;
         const dim3 grid(std::min(ctas, 148u * 32));
-        const cudaError_t e = vec ? launch<k_split_planes<T, P, 8>>(grid, dim3(256), 0, s, from, ld, FastDiv((uint32_t)per_row), pieces, N, pitch, planes, (long long)(plane_bytes / 2))
-                                  : launch<k_split_planes<T, P, 2>>(grid, dim3(256), 0, s, from, ld, FastDiv((uint32_t)per_row), pieces, N, pitch, planes, (long long)(plane_bytes / 2));
+        const cudaError_t e = vec ? launch<k_split_planes<T, P, true>>(grid, dim3(256), 0, s, from, ld, FastDiv((uint32_t)per_row), pieces, N, pitch, planes, (long long)(plane_bytes / 2))
+                                  : launch<k_split_planes<T, P, false>>(grid, dim3(256), 0, s, from, ld, FastDiv((uint32_t)per_row), pieces, N, pitch, planes, (long long)(plane_bytes / 2));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -500,7 +593,7 @@ int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t col
     if (!bytes) return ANAKIN_E_INVALID_ARG;
     const int rc = check_sizes(dtype, rows, cols, n);
     if (rc != ANAKIN_OK) return rc;
-    *bytes = make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8, nullptr, 1, true).bytes + 256;  // (for any dw)
+    *bytes = make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8).bytes + 256;
     return ANAKIN_OK;
 }
 
@@ -515,8 +608,8 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
     if (lddy >= (int64_t(1) << 31) || lddw >= (int64_t(1) << 40)) return ANAKIN_E_INVALID_ARG;
     if (act != ANAKIN_ACT_IDENTITY && act != ANAKIN_ACT_RELU) return ANAKIN_E_UNSUPPORTED_CFG;
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
-    const Plan p = make_plan(dtype, rows, cols, n, dy, lddy, dw, lddw, accumulate != 0);
-    if (rows > 0 && p.runs < 1) return ANAKIN_E_UNSUPPORTED_CFG;  // (months of work)
+    const Plan p = make_plan(dtype, rows, cols, n, dy, lddy);
+    if ((rows > 0 && p.runs < 1) || (long long)cols * (p.width / 32) >= (1ll << 31)) return ANAKIN_E_UNSUPPORTED_CFG;  // (months of work; dW of 275 GB)
     if (bytes < p.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     const int K = (int)cols, N = (int)n, R = (int)rows;
@@ -550,17 +643,20 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
         a.out = p.straight ? dw : part;
         a.ld = p.straight ? lddw : p.width;
         a.part_stride = (long long)K * p.width;
-        a.width = p.width;
+        a.add = p.straight && accumulate;
         a.relu = act == ANAKIN_ACT_RELU;
         a.status = dev_status;
         const cudaError_t e = p.P == 1 ? launch_wgrad_p<1>(maps, a, p, s) : p.P == 2 ? launch_wgrad_p<2>(maps, a, p, s) : launch_wgrad_p<3>(maps, a, p, s);
         if (e != cudaSuccess) return tok::fail();
     }
     if (!p.straight) {
-        const long long ctas = ((long long)K * N + 255) / 256;
-        if (launch<k_wgrad_sum>(dim3((unsigned)(ctas < 148 * 32 ? ctas : 148 * 32)), dim3(256), 0, s, (const float*)part, (long long)K * p.width, p.width, p.run, p.per_tile, rows == 0 ? 0 : p.chunks,
-                                p.tiles_m, p.pair ? 256 : 128, p.BN, K, N, dw, (long long)lddw, accumulate) != cudaSuccess)
-            return tok::fail();
+        const uint32_t per_row = (uint32_t)(p.width / 32), segments = (uint32_t)K * per_row;
+        const Parts parts = {part, (long long)K * p.width, FastDiv((uint32_t)std::max(1ll, p.run)), p.per_tile, p.chunks, p.tiles_m, p.pair ? 8 : 7,
+                             p.BN == 256 ? 8 : p.BN == 128 ? 7 : 6, p.width};
+        // (a dW of few segments leaves most of the GPU's warps free for the parts)
+        const cudaError_t e = p.parts > 4 && segments < 148 * 32 ? launch<k_wgrad_sum<8>>(dim3(std::min(segments, 148u * 64)), dim3(256), 0, s, parts, FastDiv(per_row), segments, N, dw, (long long)lddw, accumulate)
+                                          : launch<k_wgrad_sum<1>>(dim3(std::min((segments + 31) / 32, 148u * 16)), dim3(256), 0, s, parts, FastDiv(per_row), segments, N, dw, (long long)lddw, accumulate);
+        if (e != cudaSuccess) return tok::fail();
     }
     return ANAKIN_OK;
 }
