@@ -61,10 +61,10 @@ Workspace carve(void* base, long long rows, long long sequences) {
     size_t off = 0;
     auto take = [&](size_t bytes) { void* p = static_cast<unsigned char*>(base) + off; off += (bytes + 255) / 256 * 256; return p; };
     Workspace w;
-    w.counts = static_cast<Counts*>(take(sizeof(Counts)));
-    w.part = static_cast<double*>(take(sizeof(double) * kMaxPartials * kPolicyParts));
     const size_t parts = (size_t)sequences * prefer_splits(rows, sequences);
-    w.per_seq = static_cast<int*>(take(sizeof(int) * parts));
+    w.counts = static_cast<Counts*>(take(sizeof(Counts) + sizeof(int) * parts));
+    w.per_seq = reinterpret_cast<int*>(w.counts + 1);
+    w.part = static_cast<double*>(take(sizeof(double) * kMaxPartials * kPolicyParts));
     w.sums = static_cast<double*>(take(sizeof(double) * parts));
     w.coef = static_cast<float*>(take(sizeof(float) * (size_t)sequences));
     w.info = static_cast<int2*>(take(sizeof(int2) * (size_t)rows));
@@ -87,23 +87,91 @@ __device__ __forceinline__ void add_counts(bool counts, int seq, unsigned long l
     if (lane == __ffs(same) - 1 && atomicAdd(&per_seq[seq], __popc(same)) == 0) atomicAdd(seqs, 1ull);
 }
 
+// sequence_of(r) for a row that is known to lie in sequence `from` or behind it.
+__device__ __forceinline__ int sequence_from(const Rows& q, int from, long long r) {
+    if (from >= q.sequences || load_int(q.offsets, from + 1, q.offset_bytes) > r) return from;
+    int lo = from + 2, hi = q.sequences + 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (load_int(q.offsets, mid, q.offset_bytes) <= r) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo - 1;
+}
+// sequence_of(r) by a whole warp, which probes 32 offsets at once: three loads one after the other for thousands of sequences.
+__device__ __forceinline__ int warp_sequence_of(const Rows& q, long long r) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = q.sequences + 1;  // the number of offsets <= r lies in [lo, hi]
+    while (hi - lo > 32) {
+        const int at = lo + (int)((long long)(hi - lo) * (lane + 1) / 33);
+        const int n = __popc(__ballot_sync(0xFFFFFFFFu, load_int(q.offsets, at, q.offset_bytes) <= r));
+        const int below = __shfl_sync(0xFFFFFFFFu, at, n > 0 ? n - 1 : 0), above = __shfl_sync(0xFFFFFFFFu, at, n < 32 ? n : 31);
+        if (n > 0) lo = below + 1;
+        if (n < 32) hi = above;
+    }
+    lo += __popc(__ballot_sync(0xFFFFFFFFu, lane < hi - lo && load_int(q.offsets, lo + lane, q.offset_bytes) <= r));
+    return lo - 1;
+}
+// The sequences of the rows r0 + lane.
+__device__ __forceinline__ int warp_sequences(const Rows& q, long long r0) {
+    return q.offsets ? sequence_from(q, warp_sequence_of(q, r0), r0 + (threadIdx.x & 31)) : 0;
+}
+
+// (a kernel, as a copy engine's memset would wait for all before it and be waited for: 65536 rows 12.3 us with it, 8.4 so)
+__global__ void __launch_bounds__(256) k_zero_counts(Counts* c, int* per_seq, int sequences) {
+    PDL_START();
+    const int i0 = blockIdx.x * 256 + threadIdx.x;
+    if (i0 == 0) *c = Counts{0ull, 0ull};
+    for (long long i = i0; i < sequences; i += (long long)gridDim.x * 256) per_seq[i] = 0;
+}
+
+constexpr int kCountSteps = 4;  // groups of 32 rows, one behind the other, that a warp counts at least before it adds to the sums in memory
+
 __global__ void __launch_bounds__(256) k_token_counts(Rows q, Counts* c, int* per_seq, int2* info) {
     pdl_wait();  // (no early trigger: blocks of the next kernel placed around this one's would leave its clusters without room, a wave late)
-    const long long stride = (long long)gridDim.x * 256;
-    for (long long r0 = (long long)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < q.rows; r0 += stride) {
-        const long long r = r0 + (threadIdx.x & 31);
+    __shared__ unsigned total;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const long long groups = (q.rows + 31) / 32, warps = (long long)gridDim.x * 8, each = (groups + warps - 1) / warps;
+    const long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * each, last = min(first + each, groups);
+    int from = 0;  // the sequence of the last row looked at
+    int held = -1, n = 0;  // rows of one sequence that are not yet added to its count
+    unsigned rows = 0;
+    auto add = [&]() {
+        if (lane == 0 && n > 0 && atomicAdd(&per_seq[held], n) == 0) atomicAdd(&c->sequences, 1ull);
+    };
+    if (first < last && q.offsets) from = warp_sequence_of(q, first * 32);
+    for (long long g = first; g < last; ++g) {
+        const long long r = g * 32 + lane;
         bool counts = r < q.rows && row_counts(q, r);
-        int seq = 0;
-        if (counts) {
-            seq = sequence_of(q, r);
-            counts = seq >= 0 && seq < q.sequences;
-            if (!counts) seq = -1;
-        } else {
-            seq = -2;
-        }
+        const int found = q.offsets ? sequence_from(q, from, min(r, q.rows - 1)) : 0;
+        from = __shfl_sync(0xFFFFFFFFu, found, 31);
+        const int seq = !counts ? -2 : found >= 0 && found < q.sequences ? found : -1;
         if (info && r < q.rows) info[r] = make_int2(seq, q.tokens && seq > -2 ? (int)min(load_int(q.tokens, r, q.token_bytes), 0x7FFFFFFFll) : 0);
-        if (c) add_counts(counts, seq, &c->rows, &c->sequences, per_seq);
+        counts = seq >= 0;
+        const unsigned in = __ballot_sync(0xFFFFFFFFu, counts);
+        if (!in || !c) continue;
+        rows += __popc(in);
+        if (!per_seq) continue;
+        const int one = __shfl_sync(0xFFFFFFFFu, seq, __ffs(in) - 1);
+        if (__ballot_sync(0xFFFFFFFFu, seq == one) == in) {
+            if (one != held) {
+                add();
+                held = one;
+                n = 0;
+            }
+            n += __popc(in);
+        } else if (counts) {
+            const unsigned same = __match_any_sync(in, seq);
+            if (lane == __ffs(same) - 1 && atomicAdd(&per_seq[seq], __popc(same)) == 0) atomicAdd(&c->sequences, 1ull);
+        }
     }
+    if (!c) return;
+    if (per_seq) add();
+    if (lane == 0) atomicAdd(&total, rows);
+    __syncthreads();
+    if (threadIdx.x == 0 && total > 0) atomicAdd(&c->rows, (unsigned long long)total);
 }
 
 __device__ __forceinline__ void write_stats(const Objective& o, const double (&v)[kPolicyParts], float* stats) {
@@ -154,7 +222,7 @@ __device__ __forceinline__ void policy_row(const PolicyArgs2& A, long long r, in
     A.dlogp[r] = g;
     if (A.dentropy) A.dentropy[r] = h;
 }
-__device__ __forceinline__ int loss_sequence(const Rows& q, long long r, const int* near = nullptr) {
+__device__ __forceinline__ int loss_sequence(const Rows& q, long long r, const int* near) {
     if (!row_counts(q, r)) return -1;
     const int seq = sequence_of(q, r, near);
     return seq < q.sequences ? seq : -1;
@@ -164,8 +232,11 @@ __global__ void __launch_bounds__(256) k_policy_loss(PolicyArgs2 A) {
     PDL_START();
     __shared__ double red[8 * kPolicyParts];
     double part[kPolicyParts] = {0.0, 0.0, 0.0, 0.0, 0.0};
-    for (long long r = (long long)blockIdx.x * 256 + threadIdx.x; r < A.q.rows; r += (long long)gridDim.x * 256)
-        policy_row(A, r, loss_sequence(A.q, r), A.counts, A.per_seq, part);
+    for (long long r0 = (long long)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < A.q.rows; r0 += (long long)gridDim.x * 256) {
+        const long long r = r0 + (threadIdx.x & 31);
+        const int seq = warp_sequences(A.q, r0);
+        if (r < A.q.rows) policy_row(A, r, seq < A.q.sequences && row_counts(A.q, r) ? seq : -1, A.counts, A.per_seq, part);
+    }
     block_sums(part, red);
     if (threadIdx.x == 0) {
 #pragma unroll
@@ -354,26 +425,39 @@ __global__ void __launch_bounds__(1024) k_prefer_pairs(PreferArgs A) {
         A.coef[p + A.P] = (float)(A.sums[(size_t)(p + A.P) * A.splits] / pairs);
     }
 }
-__device__ __forceinline__ float prefer_gradient(const PreferArgs& A, long long r, const float* coef, const int* near) {
-    if (!row_counts(A.q, r)) return 0.f;
+// A row's sequence, -1 for none that counts.
+__device__ __forceinline__ int prefer_sequence(const PreferArgs& A, long long r, const int* near) {
+    if (!row_counts(A.q, r)) return -1;
     const int seq = sequence_of(A.q, r, near);
-    return seq >= 0 && seq < 2 * A.P ? coef[seq] : 0.f;
+    return seq < 2 * A.P ? seq : -1;
 }
 __global__ void __launch_bounds__(256) k_prefer_rows(PreferArgs A) {
     PDL_START();
-    for (long long r = (long long)blockIdx.x * 256 + threadIdx.x; r < A.q.rows; r += (long long)gridDim.x * 256) A.dlogp[r] = prefer_gradient(A, r, A.coef, nullptr);
+    for (long long r0 = (long long)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < A.q.rows; r0 += (long long)gridDim.x * 256) {
+        const long long r = r0 + (threadIdx.x & 31);
+        const int seq = warp_sequences(A.q, r0);
+        if (r < A.q.rows) A.dlogp[r] = seq >= 0 && seq < 2 * A.P && row_counts(A.q, r) ? A.coef[seq] : 0.f;
+    }
 }
 
 // Both for up to kFewPairs pairs: every CTA takes all pairs for itself, one a thread, instead of waiting for a kernel of one CTA (256 pairs, 262144
 // rows: 13.4 us with it, 11.0 without).
 constexpr int kFewPairs = 1024;
 __global__ void __launch_bounds__(1024) k_prefer_few(PreferArgs A) {
-    PDL_START();
+    if (A.P == 0) pdl_wait();  // (no sums before it)
     __shared__ double red[32 * 6];
     __shared__ double pairs;
     __shared__ float coef[2 * kFewPairs];
     __shared__ int offsets[2 * kFewPairs + 1];
+    // While the sums are still on their way: the sequences of the thread's first rows.  (k_prefer_sums lets this kernel start once all before it is
+    // complete, so offsets, mask and tokens are.)
     const int* near = fetch_offsets(A.q, offsets);
+    __syncthreads();
+    const long long r0 = (long long)blockIdx.x * 1024 + threadIdx.x, step = (long long)gridDim.x * 1024;
+    int seq[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) seq[k] = r0 + k * step < A.q.rows ? prefer_sequence(A, r0 + k * step, near) : -1;
+    PDL_START();
     double v[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0}, z = 0.0, d0 = 0.0, d1 = 0.0;
     const int p = threadIdx.x;
     if (p < A.P) take_pair(A, p, v, z, d0, d1);
@@ -389,7 +473,13 @@ __global__ void __launch_bounds__(1024) k_prefer_few(PreferArgs A) {
         coef[p + A.P] = (float)(d1 / pairs);
     }
     __syncthreads();
-    for (long long r = (long long)blockIdx.x * 1024 + threadIdx.x; r < A.q.rows; r += (long long)gridDim.x * 1024) A.dlogp[r] = prefer_gradient(A, r, coef, near);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (r0 + k * step < A.q.rows) A.dlogp[r0 + k * step] = seq[k] >= 0 ? coef[seq[k]] : 0.f;
+    for (long long r = r0 + 2 * step; r < A.q.rows; r += step) {
+        const int of = prefer_sequence(A, r, near);
+        A.dlogp[r] = of >= 0 ? coef[of] : 0.f;
+    }
 }
 
 int grid_for(long long rows, int per_cta, int most) {
@@ -399,14 +489,17 @@ int grid_for(long long rows, int per_cta, int most) {
 
 }  // namespace
 
-cudaError_t launch_counts(const Rows& q, int mean, const Workspace& w, cudaStream_t s) {
+cudaError_t launch_counts(const Rows& q, int mean, bool rows_too, const Workspace& w, cudaStream_t s) {
     const bool by_seq = mean == ANAKIN_MEAN_SEQUENCE;
-    cudaError_t e = cudaSuccess;
-    if (mean != ANAKIN_MEAN_FIXED) e = cudaMemsetAsync(w.counts, 0, sizeof(Counts), s);
-    if (e == cudaSuccess && by_seq && q.sequences > 0) e = cudaMemsetAsync(w.per_seq, 0, sizeof(int) * (size_t)q.sequences, s);
-    if (e != cudaSuccess) return e;
-    return launch<k_token_counts>(dim3(grid_for(q.rows, 256, 148 * 8)), dim3(256), 0, s, q, mean != ANAKIN_MEAN_FIXED ? w.counts : nullptr,
-                                  by_seq ? w.per_seq : nullptr, w.info);
+    if (mean != ANAKIN_MEAN_FIXED) {
+        const int seqs = by_seq ? q.sequences : 0;
+        const cudaError_t e = launch<k_zero_counts>(dim3(grid_for(seqs, 1024, 148)), dim3(256), 0, s, w.counts, w.per_seq, seqs);
+        if (e != cudaSuccess) return e;
+    } else if (!rows_too) {
+        return cudaSuccess;
+    }
+    return launch<k_token_counts>(dim3(grid_for(q.rows, 256 * kCountSteps, 148 * 8)), dim3(256), 0, s, q, mean != ANAKIN_MEAN_FIXED ? w.counts : nullptr,
+                                  by_seq ? w.per_seq : nullptr, rows_too ? w.info : nullptr);
 }
 
 cudaError_t launch_policy_stats(const double* part, int n, const Objective& o, float* stats, cudaStream_t s) {
@@ -454,7 +547,7 @@ int anakin_token_policy_loss(const anakin_token_rows* rows, const anakin_policy_
     if (A.q.rows <= kSmallRows && A.q.sequences <= kSmallSeqs) {
         return launch<k_policy_loss_small>(dim3(1), dim3(1024), 0, s, A) == cudaSuccess ? ANAKIN_OK : fail();
     }
-    if (A.o.mean != ANAKIN_MEAN_FIXED && launch_counts(A.q, A.o.mean, w, s) != cudaSuccess) return fail();
+    if (launch_counts(A.q, A.o.mean, false, w, s) != cudaSuccess) return fail();
     const int grid = grid_for(A.q.rows, 256, kMaxPartials);
     if (launch<k_policy_loss>(dim3(grid), dim3(256), 0, s, A) != cudaSuccess) return fail();
     return launch_policy_stats(w.part, grid, A.o, stats, s) == cudaSuccess ? ANAKIN_OK : fail();

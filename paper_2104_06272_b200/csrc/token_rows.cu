@@ -950,7 +950,7 @@ int anakin_token_policy_grad(const anakin_token_rows* rows, const anakin_policy_
     A.info = w.info;
     int grid = 0;
     if (!empty) {
-        if (launch_counts(A.q, A.o.mean, w, s) != cudaSuccess) return fail();
+        if (launch_counts(A.q, A.o.mean, true, w, s) != cudaSuccess) return fail();
         if (launch_rows_any<FUSED>(rows->dtype, A, &grid, s) != cudaSuccess) return fail();
     }
     return launch_policy_stats(w.part, grid, A.o, stats, s) == cudaSuccess ? ANAKIN_OK : fail();

@@ -84,13 +84,13 @@ struct Rows {
 };
 
 // The sequence of row r: the last i with offsets[i] <= r; -1 before the first and `sequences` behind the last.  Any offsets give a
-// number in that range.  `near`: the offsets as 32-bit numbers in shared memory, or null.
-__device__ __forceinline__ int sequence_of(const Rows& q, long long r, const int* near = nullptr) {
+// number in that range.  `near`: the offsets as 32-bit numbers in shared memory.
+__device__ __forceinline__ int sequence_of(const Rows& q, long long r, const int* near) {
     if (!q.offsets) return 0;
     int lo = 0, hi = q.sequences + 1;  // the number of offsets <= r lies in [lo, hi]
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if ((near ? (long long)near[mid] : load_int(q.offsets, mid, q.offset_bytes)) <= r) lo = mid + 1;
+        if (near[mid] <= r) lo = mid + 1;
         else hi = mid;
     }
     return lo - 1;
@@ -180,8 +180,8 @@ constexpr int kMaxPartials = 148 * 16;  // CTAs that may leave some
 // Layout of the workspace of the losses.
 struct Workspace {
     Counts* counts;
+    int* per_seq;   // [sequences] (of the preference loss: times its splits), right behind the counts
     double* part;   // [kMaxPartials][kPolicyParts]
-    int* per_seq;   // [sequences] (of the preference loss: times its splits)
     double* sums;   // [sequences times splits] of the preference loss
     float* coef;    // [sequences] of the preference loss
     int2* info;     // [rows] of the policy gradient: the row's sequence (-1: no part in the loss, -2: does not count at all) and its token
@@ -189,8 +189,8 @@ struct Workspace {
 };
 Workspace carve(void* base, long long rows, long long sequences);
 
-// What the means divide by (ANAKIN_MEAN_*), and every row's sequence, into the workspace.
-cudaError_t launch_counts(const Rows& q, int mean, const Workspace& w, cudaStream_t s);
+// What the means divide by (ANAKIN_MEAN_*) and, with rows_too, every row's sequence and token, into the workspace.
+cudaError_t launch_counts(const Rows& q, int mean, bool rows_too, const Workspace& w, cudaStream_t s);
 
 // Host: checks of what every call has in common; fills q.
 int check_rows(const anakin_token_rows* rows, bool need_logits, bool need_tokens, bool need_offsets, Rows* q);
