@@ -1,5 +1,5 @@
 // Weight gradient of a layer from its input's 8-bit checkpoint:  dW[k][n] (+)= sum_r f(x[r][k]) dY[r][n],  f = identity or ReLU, on the
-// 5th-generation tensor cores.
+// 5th-generation tensor cores (with 32 rows or fewer: k_wgrad_few).
 //
 // A kept value is an e4m3 number times a power of two: exact in bf16.  dY is one bf16 term, or two (fp16) or three (fp32) that sum to it, in planes
 // that a first kernel writes.  So every product is exact in the MMA and the sums are the only rounding.  Both operands have the contraction index r
@@ -465,6 +465,66 @@ __global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld,
     }
 }
 
+// Up to 32 rows: what there is to do is to write dW, and setting tensor cores up costs more than the products (4 x 1024 x 32768 bf16: 27 us, by tensor
+// cores 82; 32 rows 77; 32 x 1024 x 1024 7.7 and 11.8; with 48 rows tensor cores are ahead where tiles are many).  A CTA takes 64 rows of dW x 128
+// columns, a warp 8 rows, a lane 4 columns of them 32 apart.  Sums in the order of the rows, fp32, one rounding a product.
+constexpr int kFewRows = 32, kFewK = 64, kFewN = 128;
+template <class T>
+__global__ void __launch_bounds__(256) k_wgrad_few(const uint8_t* codes, const uint8_t* scales, const T* dy, long long lddy, int R, int K, int N, int blocks, uint32_t tiles_n,
+                                                   int relu, float* dw, long long lddw, int add) {
+    PDL_START();
+    __shared__ __align__(16) float xs[kFewRows][kFewK];
+    __shared__ float ys[kFewRows][kFewN];
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const uint32_t on = relu ? 0xFFFFFFFFu : 0u;
+    const int k0 = (int)(blockIdx.x / tiles_n) * kFewK, n0 = (int)(blockIdx.x % tiles_n) * kFewN;
+    float v[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+    const int xr = tid >> 3, xk = k0 + (tid & 7) * 8;
+    if (xr < R && xk < blocks * 32) {
+        uint2 q = *reinterpret_cast<const uint2*>(codes + (size_t)xr * blocks * 32 + xk);
+        q = make_uint2(relu_codes(q.x, on), relu_codes(q.y, on));
+        float f[8];
+        decode8(q, scales[(size_t)xr * blocks + xk / 32], f);
+        float4* to = reinterpret_cast<float4*>(&xs[xr][xk - k0]);
+        to[0] = make_float4(f[0], f[1], f[2], f[3]);
+        to[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    const int c = tid & 127;
+#pragma unroll
+    for (int i = 0; i < kFewRows / 2; ++i) {
+        const int r = 2 * i + (tid >> 7);
+        if (r < R) ys[r][c] = n0 + c < N ? tok::to_f(dy[(long long)r * lddy + n0 + c]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int r = 0; r < R; ++r) {
+        const float4 a = *reinterpret_cast<const float4*>(&xs[r][8 * wid]), b = *reinterpret_cast<const float4*>(&xs[r][8 * wid + 4]);
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float y = ys[r][32 * j + lane];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i][j] = fmaf(x[i], y, v[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = k0 + 8 * wid + i;
+        float* row = dw + (long long)k * lddw + n0 + lane;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (k < K && n0 + 32 * j + lane < N) row[32 * j] = add ? row[32 * j] + v[i][j] : v[i][j];
+    }
+}
+template <class T>
+cudaError_t launch_few(const uint8_t* codes, const uint8_t* scales, const void* dy, long long lddy, int R, int K, int N, int relu, float* dw, long long lddw, int add, cudaStream_t s) {
+    const uint32_t tiles_n = (uint32_t)((N + kFewN - 1) / kFewN), tiles = tiles_n * (uint32_t)((K + kFewK - 1) / kFewK);
+    return launch<k_wgrad_few<T>>(dim3(tiles), dim3(256), 0, s, codes, scales, static_cast<const T*>(dy), lddy, R, K, N, (K + 31) / 32, tiles_n, relu, dw, lddw, add);
+}
 struct Plan {
     int P, BN, pitch, width, runs, per_tile, tiles_m, tiles, chunks, parts;  // parts: the most runs that share a tile; width: floats of a partial row
     long long run, total;
@@ -593,7 +653,7 @@ int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t col
     if (!bytes) return ANAKIN_E_INVALID_ARG;
     const int rc = check_sizes(dtype, rows, cols, n);
     if (rc != ANAKIN_OK) return rc;
-    *bytes = make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8).bytes + 256;
+    *bytes = rows > 0 && rows <= kFewRows ? 256 : make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8).bytes + 256;
     return ANAKIN_OK;
 }
 
@@ -608,6 +668,15 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
     if (lddy >= (int64_t(1) << 31) || lddw >= (int64_t(1) << 40)) return ANAKIN_E_INVALID_ARG;
     if (act != ANAKIN_ACT_IDENTITY && act != ANAKIN_ACT_RELU) return ANAKIN_E_UNSUPPORTED_CFG;
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
+    if (rows > 0 && rows <= kFewRows) {
+        if ((cols + kFewK - 1) / kFewK * ((n + kFewN - 1) / kFewN) >= (int64_t(1) << 31)) return ANAKIN_E_UNSUPPORTED_CFG;
+        cudaStream_t st = (cudaStream_t)cuda_stream;
+        const int few_relu = act == ANAKIN_ACT_RELU;
+        const cudaError_t e = dtype == ANAKIN_DTYPE_F32 ? launch_few<float>(codes, scales, dy, lddy, (int)rows, (int)cols, (int)n, few_relu, dw, lddw, accumulate, st)
+                              : dtype == ANAKIN_DTYPE_F16 ? launch_few<__half>(codes, scales, dy, lddy, (int)rows, (int)cols, (int)n, few_relu, dw, lddw, accumulate, st)
+                                                          : launch_few<__nv_bfloat16>(codes, scales, dy, lddy, (int)rows, (int)cols, (int)n, few_relu, dw, lddw, accumulate, st);
+        return e == cudaSuccess ? ANAKIN_OK : tok::fail();
+    }
     const Plan p = make_plan(dtype, rows, cols, n, dy, lddy);
     if ((rows > 0 && p.runs < 1) || (long long)cols * (p.width / 32) >= (1ll << 31)) return ANAKIN_E_UNSUPPORTED_CFG;  // (months of work; dW of 275 GB)
     if (bytes < p.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
