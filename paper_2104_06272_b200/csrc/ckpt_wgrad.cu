@@ -1,5 +1,5 @@
 // Weight gradient of a layer from its input's 8-bit checkpoint:  dW[k][n] (+)= sum_r f(x[r][k]) dY[r][n],  f = identity or ReLU, on the
-// 5th-generation tensor cores (with 32 rows or fewer: k_wgrad_few).
+// 5th-generation tensor cores (small ones: k_wgrad_few).
 //
 // A kept value is an e4m3 number times a power of two: exact in bf16.  dY is one bf16 term, or two (fp16) or three (fp32) that sum to it, in planes
 // that a first kernel writes.  So every product is exact in the MMA and the sums are the only rounding.  Both operands have the contraction index r
@@ -468,13 +468,20 @@ __global__ void __launch_bounds__(256) k_split_planes(const T* dy, long long ld,
 // Up to 32 rows: what there is to do is to write dW, and setting tensor cores up costs more than the products (4 x 1024 x 32768 bf16: 27 us, by tensor
 // cores 82; 32 rows 77; 32 x 1024 x 1024 7.7 and 11.8; with 48 rows tensor cores are ahead where tiles are many).  A CTA takes 64 rows of dW x 128
 // columns, a warp 8 rows, a lane 4 columns of them 32 apart.  Sums in the order of the rows, fp32, one rounding a product.
-constexpr int kFewRows = 32, kFewK = 64, kFewN = 128;
-template <class T>
+// More rows while dW is small, too: 16 of them to a CTA (blockIdx.y), partial sums as from the tensor cores' runs (1024 x 64 x 64 fp32: 5.9 us, with 32
+// rows 9.0, by tensor cores 9.9; 640 x 256 x 256 bf16 11.9, 13.2 and 14.7).
+constexpr int kFewRows = 32, kSplitRows = 16, kFewK = 64, kFewN = 128;
+template <class T, int ROWS>
 __global__ void __launch_bounds__(256) k_wgrad_few(const uint8_t* codes, const uint8_t* scales, const T* dy, long long lddy, int R, int K, int N, int blocks, uint32_t tiles_n,
-                                                   int relu, float* dw, long long lddw, int add) {
+                                                   int relu, float* dw, long long lddw, long long part_stride, int add) {
     PDL_START();
-    __shared__ __align__(16) float xs[kFewRows][kFewK];
-    __shared__ float ys[kFewRows][kFewN];
+    codes += (size_t)blockIdx.y * ROWS * blocks * 32;
+    scales += (size_t)blockIdx.y * ROWS * blocks;
+    dy += (long long)blockIdx.y * ROWS * lddy;
+    dw += blockIdx.y * part_stride;
+    R = min(R - (int)blockIdx.y * ROWS, ROWS);
+    __shared__ __align__(16) float xs[ROWS][kFewK];
+    __shared__ float ys[ROWS][kFewN];
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const uint32_t on = relu ? 0xFFFFFFFFu : 0u;
     const int k0 = (int)(blockIdx.x / tiles_n) * kFewK, n0 = (int)(blockIdx.x % tiles_n) * kFewN;
@@ -495,7 +502,7 @@ __global__ void __launch_bounds__(256) k_wgrad_few(const uint8_t* codes, const u
     }
     const int c = tid & 127;
 #pragma unroll
-    for (int i = 0; i < kFewRows / 2; ++i) {
+    for (int i = 0; i < ROWS / 2; ++i) {
         const int r = 2 * i + (tid >> 7);
         if (r < R) ys[r][c] = n0 + c < N ? tok::to_f(dy[(long long)r * lddy + n0 + c]) : 0.f;
     }
@@ -520,11 +527,28 @@ __global__ void __launch_bounds__(256) k_wgrad_few(const uint8_t* codes, const u
             if (k < K && n0 + 32 * j + lane < N) row[32 * j] = add ? row[32 * j] + v[i][j] : v[i][j];
     }
 }
-template <class T>
-cudaError_t launch_few(const uint8_t* codes, const uint8_t* scales, const void* dy, long long lddy, int R, int K, int N, int relu, float* dw, long long lddw, int add, cudaStream_t s) {
-    const uint32_t tiles_n = (uint32_t)((N + kFewN - 1) / kFewN), tiles = tiles_n * (uint32_t)((K + kFewK - 1) / kFewK);
-    return launch<k_wgrad_few<T>>(dim3(tiles), dim3(256), 0, s, codes, scales, static_cast<const T*>(dy), lddy, R, K, N, (K + 31) / 32, tiles_n, relu, dw, lddw, add);
+// CTAs that share the rows, 0 for work of the tensor cores: one for 32 rows at most, more while all tiles are at work at once.
+int few_splits(long long R, long long K, long long N) {
+    const long long splits = (R + kSplitRows - 1) / kSplitRows, tiles = ((K + kFewK - 1) / kFewK) * ((N + kFewN - 1) / kFewN);
+    return R <= kFewRows ? 1 : splits <= 128 && tiles * splits <= 148 * 4 ? (int)splits : 0;
 }
+int partial_width(long long N) { return (int)((N + 31) / 32 * 32); }
+template <class T>
+cudaError_t launch_few(const uint8_t* codes, const uint8_t* scales, const void* dy, long long lddy, int splits, int R, int K, int N, int relu, float* dw, long long lddw,
+                       long long part_stride, int add, cudaStream_t s) {
+    const uint32_t tiles_n = (uint32_t)((N + kFewN - 1) / kFewN), tiles = tiles_n * (uint32_t)((K + kFewK - 1) / kFewK);
+    const dim3 grid(tiles, splits), block(256);
+    return splits == 1 ? launch<k_wgrad_few<T, kFewRows>>(grid, block, 0, s, codes, scales, static_cast<const T*>(dy), lddy, R, K, N, (K + 31) / 32, tiles_n, relu, dw, lddw, part_stride, add)
+                       : launch<k_wgrad_few<T, kSplitRows>>(grid, block, 0, s, codes, scales, static_cast<const T*>(dy), lddy, R, K, N, (K + 31) / 32, tiles_n, relu, dw, lddw, part_stride, add);
+}
+// (parts: the most that any element has)
+cudaError_t launch_sum(const Parts& p, int parts, int K, int N, float* dw, long long lddw, int add, cudaStream_t s) {
+    const uint32_t per_row = (uint32_t)(p.pitch / 32), segments = (uint32_t)K * per_row;
+    // (a dW of few segments leaves most of the GPU's warps free for the parts)
+    return parts > 4 && segments < 148 * 32 ? launch<k_wgrad_sum<8>>(dim3(segments), dim3(256), 0, s, p, FastDiv(per_row), segments, N, dw, lddw, add)
+                                            : launch<k_wgrad_sum<1>>(dim3(std::min((segments + 31) / 32, 148u * 16)), dim3(256), 0, s, p, FastDiv(per_row), segments, N, dw, lddw, add);
+}
+
 struct Plan {
     int P, BN, pitch, width, runs, per_tile, tiles_m, tiles, chunks, parts;  // parts: the most runs that share a tile; width: floats of a partial row
     long long run, total;
@@ -550,7 +574,7 @@ Plan make_plan(int dtype, long long R, long long K, long long N, const void* dy,
     // Or runs of the same length go on from tile to tile and every SM is busy; then, where codes and dY are more than L2 holds, each tile reads its
     // own from memory.  A run has four chunks at least; a chunk takes some 0.47 us (one term; 0.3 a term with more), a MB of partial sums written
     // and read 0.5 us, a kernel or another wave of runs 2.
-    p.width = (int)((N + 31) / 32 * 32);
+    p.width = partial_width(N);
     if (p.chunks == 0) return p;
     const double us = p.P == 1 ? 0.47 : 0.3 * p.P, part_us = 2e-6 * (double)K * (double)N;
     const double tiles_n = (double)((N + p.BN - 1) / p.BN), code_mb = 1e-6 * R * K, dy_mb = 2e-6 * R * N * p.P;
@@ -653,7 +677,8 @@ int anakin_ckpt_weight_grad_workspace_bytes(int dtype, int64_t rows, int64_t col
     if (!bytes) return ANAKIN_E_INVALID_ARG;
     const int rc = check_sizes(dtype, rows, cols, n);
     if (rc != ANAKIN_OK) return rc;
-    *bytes = rows > 0 && rows <= kFewRows ? 256 : make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8).bytes + 256;
+    const int splits = rows > 0 ? few_splits(rows, cols, n) : 0;
+    *bytes = splits > 0 ? 256 + (splits > 1 ? sizeof(float) * splits * (size_t)cols * partial_width(n) : 0) : make_plan(dtype, rows, cols, n, reinterpret_cast<const void*>((uintptr_t)(dy_aligned ? 16 : 1)), 8).bytes + 256;
     return ANAKIN_OK;
 }
 
@@ -668,20 +693,24 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
     if (lddy >= (int64_t(1) << 31) || lddw >= (int64_t(1) << 40)) return ANAKIN_E_INVALID_ARG;
     if (act != ANAKIN_ACT_IDENTITY && act != ANAKIN_ACT_RELU) return ANAKIN_E_UNSUPPORTED_CFG;
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
-    if (rows > 0 && rows <= kFewRows) {
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    const int K = (int)cols, N = (int)n, R = (int)rows;
+    if (const int splits = rows > 0 ? few_splits(rows, cols, n) : 0) {
         if ((cols + kFewK - 1) / kFewK * ((n + kFewN - 1) / kFewN) >= (int64_t(1) << 31)) return ANAKIN_E_UNSUPPORTED_CFG;
-        cudaStream_t st = (cudaStream_t)cuda_stream;
-        const int few_relu = act == ANAKIN_ACT_RELU;
-        const cudaError_t e = dtype == ANAKIN_DTYPE_F32 ? launch_few<float>(codes, scales, dy, lddy, (int)rows, (int)cols, (int)n, few_relu, dw, lddw, accumulate, st)
-                              : dtype == ANAKIN_DTYPE_F16 ? launch_few<__half>(codes, scales, dy, lddy, (int)rows, (int)cols, (int)n, few_relu, dw, lddw, accumulate, st)
-                                                          : launch_few<__nv_bfloat16>(codes, scales, dy, lddy, (int)rows, (int)cols, (int)n, few_relu, dw, lddw, accumulate, st);
+        const int relu = act == ANAKIN_ACT_RELU, width = partial_width(n), direct = splits == 1;
+        const long long stride = (long long)cols * width;
+        if (!direct && bytes < sizeof(float) * splits * (size_t)stride) return ANAKIN_E_WORKSPACE_TOO_SMALL;
+        float* part = static_cast<float*>(dev_workspace);
+        auto run = [&](auto type) {
+            return launch_few<decltype(type)>(codes, scales, dy, lddy, splits, R, K, N, relu, direct ? dw : part, direct ? lddw : width, stride, direct && accumulate, s);
+        };
+        cudaError_t e = dtype == ANAKIN_DTYPE_F32 ? run(float{}) : dtype == ANAKIN_DTYPE_F16 ? run(__half{}) : run(__nv_bfloat16{});
+        if (e == cudaSuccess && !direct) e = launch_sum(Parts{part, stride, FastDiv(1), splits, 1, 1, 0, 0, width}, splits, K, N, dw, lddw, accumulate, s);
         return e == cudaSuccess ? ANAKIN_OK : tok::fail();
     }
     const Plan p = make_plan(dtype, rows, cols, n, dy, lddy);
     if ((rows > 0 && p.runs < 1) || (long long)cols * (p.width / 32) >= (1ll << 31)) return ANAKIN_E_UNSUPPORTED_CFG;  // (months of work; dW of 275 GB)
     if (bytes < p.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    const int K = (int)cols, N = (int)n, R = (int)rows;
     float* part = reinterpret_cast<float*>(static_cast<unsigned char*>(dev_workspace) + p.part_off);
     if (rows > 0) {
         Maps maps;
@@ -719,12 +748,9 @@ int anakin_ckpt_weight_grad(int dtype, int act, int64_t rows, int64_t cols, int6
         if (e != cudaSuccess) return tok::fail();
     }
     if (!p.straight) {
-        const uint32_t per_row = (uint32_t)(p.width / 32), segments = (uint32_t)K * per_row;
         const Parts parts = {part, (long long)K * p.width, FastDiv((uint32_t)std::max(1ll, p.run)), p.per_tile, p.chunks, p.tiles_m, p.pair ? 8 : 7,
                              p.BN == 256 ? 8 : p.BN == 128 ? 7 : 6, p.width};
-        // (a dW of few segments leaves most of the GPU's warps free for the parts)
-        const cudaError_t e = p.parts > 4 && segments < 148 * 32 ? launch<k_wgrad_sum<8>>(dim3(std::min(segments, 148u * 64)), dim3(256), 0, s, parts, FastDiv(per_row), segments, N, dw, (long long)lddw, accumulate)
-                                          : launch<k_wgrad_sum<1>>(dim3(std::min((segments + 31) / 32, 148u * 16)), dim3(256), 0, s, parts, FastDiv(per_row), segments, N, dw, (long long)lddw, accumulate);
+        const cudaError_t e = launch_sum(parts, p.parts, K, N, dw, (long long)lddw, accumulate, s);
         if (e != cudaSuccess) return tok::fail();
     }
     return ANAKIN_OK;

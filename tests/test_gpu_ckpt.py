@@ -142,10 +142,11 @@ def wgrad_want(ck, dy, act, tk):
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("R,K,N,pad", [(1, 1, 1, 0), (1, 33, 70, 0), (5, 64, 8, 0), (63, 32, 64, 0), (64, 128, 65, 7), (65, 129, 128, 8), (1000, 200, 129, 0), (513, 96, 256, 0),
                                        (2049, 40, 257, 3), (5000, 300, 520, 8), (40000, 64, 64, 0), (300, 1030, 1000, 0), (129, 257, 263, 7), (5003, 300, 4099, 0),
-                                       (2600, 512, 2048, 0), (30000, 260, 72, 1), (32, 65, 129, 1), (17, 160, 300, 0), (33, 500, 700, 0)])
+                                       (2600, 512, 2048, 0), (30000, 260, 72, 1), (32, 65, 129, 1), (17, 160, 300, 0), (33, 500, 700, 0),
+                                       (2048, 64, 130, 3), (2049, 1, 1, 0), (3000, 33, 70, 0), (2113, 128, 65, 7), (2500, 129, 128, 8), (4100, 200, 129, 0), (50, 2100, 777, 0)])
 def test_weight_grad(tk, R, K, N, pad, dtype):
     """Products are exact; the sums: up to 32 accumulations toward zero in an accumulator (2^-23 of its size each), then one addition a group of 512
-    rows at most and one a split (2^-24 each): 2^-23 (32 + R/128) of the sum of the absolute values is a bound.  (Up to 32 rows: as many roundings of 2^-24.)"""
+    rows at most and one a split (2^-24 each): 2^-23 (32 + R/128) of the sum of the absolute values is a bound.  (Small ones: 32 roundings of 2^-24 and one for each 16 rows.)"""
     dt = DT[dtype]
     x = matrix(R, K, torch.float32, R + K, sd=0.3)
     _, ck = tk.ckpt_forward(x, "relu")
