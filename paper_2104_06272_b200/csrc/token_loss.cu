@@ -92,7 +92,7 @@ __device__ __forceinline__ int sequence_from(const Rows& q, int from, long long 
     if (from >= q.sequences || load_int(q.offsets, from + 1, q.offset_bytes) > r) return from;
     int lo = from + 2, hi = q.sequences + 1;
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);  // (their sum may pass 2^31)
         if (load_int(q.offsets, mid, q.offset_bytes) <= r) lo = mid + 1;
         else hi = mid;
     }

@@ -561,3 +561,20 @@ def test_logp_has_no_bias(tk, R, V, dtype, scale):
     l = plain.logp(x, tokens, s32)[0]
     err = (tk.logp(x, tokens, scale).logp.double() - l).mean().item()
     assert abs(err) < 2.0 ** -22 + 5 * 2.0 ** -20 / (3 * R) ** 0.5, err
+
+
+def test_more_than_2_to_the_30_sequences(tk):
+    """Nearly all of them empty: places in the offsets whose sum passes 2^31."""
+    S, R = (1 << 30) + 5, 9000
+    offsets = torch.zeros(S + 1, dtype=torch.int32, device="cuda")
+    offsets[S - 1], offsets[S] = 4010, R
+    g = torch.Generator(device="cuda").manual_seed(1)
+    l, old, adv, ref, H, _, mask = policy_inputs(R, 2, g)
+    f, obj = objective(tk, mean="sequence")
+    old = off_the_edge(f, l, old)
+    near_offsets = torch.tensor([0, 4010, R], device="cuda")
+    got = tk.policy_loss(obj, l, old, adv, ref_logp=ref, entropy=H, mask=mask, offsets=offsets)
+    check_policy(got, plain.policy(f, l, old, adv, ref, H, None, mask, near_offsets), R, float(adv[mask].abs().max()) * 10)
+    x, tokens, _ = make(R, 5, torch.float32, 3)
+    a, b = (tk.policy_grad(obj, x, tokens, old, adv, ref_logp=ref, mask=mask, offsets=o) for o in (offsets, near_offsets))
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
