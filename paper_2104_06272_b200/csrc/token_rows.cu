@@ -314,8 +314,9 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
         const int head = G > 1 ? head_of<T>(x, V) : 0;
         const int nvec = G > 1 ? (V - head) / N : 0, tail = head + nvec * N;
         const uint4* xv = reinterpret_cast<const uint4*>(x + head);
-        // the elements of a row's head and tail: the e-th
-        auto extra = [&](int e) { return e < head ? e : tail + e - head; };
+        // the elements of a row's head and tail: how many, and the e-th
+        const int extras = head + (V - tail);
+        auto extra = [&](int e) { return e < head ? e : tail + (e - head); };
         RowGrad gr;
         if constexpr (MODE != BACKWARD) {
             Acc acc;
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                         const uint4 u[1] = {xv[i]};
                         acc.template add_vectors<T>(u, c);
                     }
-                    for (int e = lane; extra(e) < V; e += G) {
+                    for (int e = lane; e < extras; e += G) {
                         const float f[2] = {to_f(x[extra(e)]), -INFINITY};
                         acc.add_scalars(f, c);
                     }
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                     store_vector(out + head + (size_t)(i + step) * N, gr.template vector<T>(u1, head + (i + step) * N, c), vec);
                 }
                 if (i < nvec) store_vector(out + head + (size_t)i * N, gr.template vector<T>(xv[i], head + i * N, c), vec);
-                for (int e = lane; blockIdx.y == 0 && extra(e) < V; e += G) out[extra(e)] = from_f<T>(gr.scalar(to_f(x[extra(e)]), extra(e), c));
+                for (int e = lane; blockIdx.y == 0 && e < extras; e += G) out[extra(e)] = from_f<T>(gr.scalar(to_f(x[extra(e)]), extra(e), c));
             }
         }
     }

@@ -578,3 +578,18 @@ def test_more_than_2_to_the_30_sequences(tk):
     x, tokens, _ = make(R, 5, torch.float32, 3)
     a, b = (tk.policy_grad(obj, x, tokens, old, adv, ref_logp=ref, mask=mask, offsets=o) for o in (offsets, near_offsets))
     assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_the_longest_vocabulary(tk):
+    """2^31 - 1 logits in a row: a column's number plus a block's threads would pass 32 bits."""
+    V = (1 << 31) - 1
+    x = torch.zeros(1 + V + 8, dtype=torch.bfloat16, device="cuda")[1: 1 + V].view(1, V)
+    tokens = torch.tensor([V - 1], device="cuda")
+    o = tk.logp(x, tokens)
+    # (the sums are counts, exact in fp32 up to 2^24 in every thread)
+    assert abs(o.logp[0].item() + math.log(V)) < 1e-5 and abs(o.entropy[0].item() - math.log(V)) < 1e-5
+    flat = torch.full((V + 17,), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = flat[3: 3 + V].view(1, V)
+    tk.logp_backward(x, tokens, o.norm, torch.ones(1, device="cuda"), out=got)
+    assert got[0, -1] == 1.0 and abs(got[0, 0].item() * V + 1.0) < 2.0 ** -8 and (got[0, :-1] == got[0, 0]).all()
+    assert (flat[:3] == 7).all() and (flat[3 + V:] == 7).all()
