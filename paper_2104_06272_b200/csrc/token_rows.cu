@@ -902,6 +902,10 @@ cudaError_t launch_rows_any(int dtype, const RowArgs& A, int* parts, cudaStream_
 using namespace anakin;
 using namespace anakin::tok;
 
+static bool bad_output(const anakin_token_rows* rows, const void* dlogits, int64_t ld_out) {
+    return ld_out < rows->vocab || (rows->rows > 0 && (!dlogits || ((uintptr_t)dlogits & (rows->dtype == ANAKIN_DTYPE_F32 ? 3 : 1))));
+}
+
 extern "C" {
 
 int anakin_token_logp(const anakin_token_rows* rows, float* logp, float* entropy, float* norm, void* cuda_stream) {
@@ -921,9 +925,9 @@ int anakin_token_logp_backward(const anakin_token_rows* rows, const float* norm,
     RowArgs A = {};
     const int rc = check_rows(rows, true, true, false, &A.q);
     if (rc != ANAKIN_OK) return rc;
-    if (ld_out < rows->vocab) return ANAKIN_E_INVALID_ARG;
+    if (bad_output(rows, dlogits, ld_out)) return ANAKIN_E_INVALID_ARG;
     if (A.q.rows == 0) return ANAKIN_OK;
-    if (!norm || !dlogp || !dlogits || (dentropy && !entropy)) return ANAKIN_E_INVALID_ARG;
+    if (!norm || !dlogp || (dentropy && !entropy)) return ANAKIN_E_INVALID_ARG;
     A.norm_in = norm;
     A.entropy_in = entropy;
     A.dlogp = dlogp;
@@ -941,7 +945,7 @@ int anakin_token_policy_grad(const anakin_token_rows* rows, const anakin_policy_
     if (rc == ANAKIN_OK) rc = check_policy(objective, &A.o);
     if (rc != ANAKIN_OK) return rc;
     const bool empty = A.q.rows == 0;
-    if (!stats || ld_out < rows->vocab || (!empty && (!adv || !dlogits || (A.o.kl != ANAKIN_KL_NONE && !ref_logp)))) return ANAKIN_E_INVALID_ARG;
+    if (!stats || bad_output(rows, dlogits, ld_out) || (!empty && (!adv || (A.o.kl != ANAKIN_KL_NONE && !ref_logp)))) return ANAKIN_E_INVALID_ARG;
     const Workspace w = carve(dev_workspace, A.q.rows, A.q.sequences);
     if (!dev_workspace || ((uintptr_t)dev_workspace & 255)) return ANAKIN_E_INVALID_ARG;
     if (bytes < w.bytes) return ANAKIN_E_WORKSPACE_TOO_SMALL;

@@ -175,3 +175,12 @@ def test_kept_values_are_the_nearest():
     assert torch.equal(got, want)
     top = x.view(40, 2, 32).abs().amax(2).double()
     assert (top <= 448 * torch.exp2(E.double())).all() and (top > 224 * torch.exp2(E.double())).all()
+
+
+def test_gradients_at_odd_addresses_are_refused(tk):
+    """As the logits are: an element's address is a multiple of its size."""
+    lib, obj = tk._lib, tk.policy_objective()
+    for dtype, at in ((0, 0x10002), (1, 0x10001), (2, 0x10003)):
+        r, out = rows_of(tk, dtype=dtype), C.c_void_p(at)
+        assert lib.anakin_token_logp_backward(C.byref(r), FAKE, FAKE, FAKE, FAKE, out, 100, None) == -1
+        assert lib.anakin_token_policy_grad(C.byref(r), C.byref(obj), FAKE, FAKE, None, FAKE, None, None, out, 100, FAKE, 1 << 30, None) == -1
