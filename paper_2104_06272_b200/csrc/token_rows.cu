@@ -4,8 +4,8 @@
 // With x the logits of a row, c = scale log2(e), m = max x, M = c m rounded, d_j = c x_j - M (one fused multiply-add):
 //   s = sum 2^d,  t = sum 2^d d   in one pass, rescaled whenever m grows;   log p_j = ln2 d_j - ln s;   H = ln s - ln2 t / s
 //   dx_j = scale ( g ([j = token] - p_j) - h p_j (log p_j + H) ) = 2^d_j ( a + b d_j ) + [j = token] scale g
-// M's rounding is the same in every term and cancels.  Where m is beyond 2^80 (a row of nothing but masks of the type's lowest value), c x would
-// overflow: there d_j = c (x_j - m).  Terms that are -inf give 2^d = 0, and 0 times d is kept from being NaN by a lower bound on d, in those
+// M's rounding is the same in every term and cancels while it is small: up to |M| = 2^22 it is 1/8 at most, and the largest term between 2^-1/8 and
+// 2^1/8.  Beyond that (a part of a row where nothing but masks stands, a large scale) it would be an exponent of any size: there d_j = c (x_j - m).  Terms that are -inf give 2^d = 0, and 0 times d is kept from being NaN by a lower bound on d, in those
 // groups of logits only that hold such a term.
 //
 // What bounds these kernels is memory or, in 16-bit types, the issue slots: an element costs an exponential and some 4 other instructions forward
@@ -78,10 +78,15 @@ template <class T, int U> __device__ __forceinline__ void extremes(const uint4 (
 }
 
 constexpr float kHuge = 1.2089258e24f;  // 2^80: times c (scale is at most 2^40) far from fp32's largest
-__device__ __forceinline__ bool usual(float m) { return fabsf(m) < kHuge; }
+// Terms are relative to M = c m rounded, not to m itself.
+__device__ __forceinline__ bool usual(float M) { return fabsf(M) < 4194304.f; }
 
-// The factor, and its logarithm to base 2, from sums relative to m to sums relative to a larger maximum.
-__device__ __forceinline__ float log_factor(float m, float to, float c) { return usual(m) && usual(to) ? __fmul_rn(m, c) - __fmul_rn(to, c) : (m - to) * c; }
+// The logarithm to base 2 of the factor from sums relative to m to sums relative to a larger maximum.
+__device__ __forceinline__ float log_factor(float m, float to, float c) {
+    const float M = __fmul_rn(m, c), T = __fmul_rn(to, c);
+    if (usual(M)) return usual(T) ? M - T : -fmaf(to, c, -M);
+    return usual(T) ? fmaf(m, c, -T) : (m - to) * c;
+}
 
 // Maximum, sum and weighted sum of a part of a row.
 struct Soft {
@@ -139,8 +144,9 @@ struct Acc {
         t = fma2(e, BOUND ? f2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)) : d, t);  // (a NaN comes through s)
     }
     template <int N> __device__ __forceinline__ void add(const float (&f)[N], float low, float c) {
-        if (usual(m)) {
-            const F2 cc = f2(c, c), off = f2(-__fmul_rn(m, c), -__fmul_rn(m, c));
+        const float M = __fmul_rn(m, c);
+        if (usual(M)) {
+            const F2 cc = f2(c, c), off = f2(-M, -M);
             if (low > -kHuge) {
 #pragma unroll
                 for (int k = 0; k < N; k += 2) term<false>(fma2(f2(f[k], f[k + 1]), cc, off));
@@ -190,15 +196,16 @@ struct Acc {
 // What the gradient of a row needs: 2^d ( a + b d ), d = c x - off or c (x - off), and `onehot` more at the token.
 struct RowGrad {
     float off, a, b, onehot;
-    int token, kind;  // kind: 0 usual, 1 = from differences (m beyond 2^80, or a short row), 2 = zeros, 3 = NaN
+    int token, kind;  // kind: 0 usual, 1 = from differences (M beyond 2^22, or a short row), 2 = zeros, 3 = NaN
     __device__ __forceinline__ void set(float m, float ln_s, float g, float h, float H, float scale, float c, long long tok, long long V, bool as_differences = false) {
         const float ls2 = ln_s * kLog2e, inv = ex2(-ls2);
         const float a0 = -scale * (g + h * H), b0 = -scale * h * kLn2;  // p ( a0 + b0 log2 p ),  p = 2^d / s
         a = (a0 - b0 * ls2) * inv;
         b = b0 * inv;
         onehot = scale * g;
-        const bool fused = usual(m) && !as_differences;
-        off = fused ? __fmul_rn(m, c) : m;
+        const float M = __fmul_rn(m, c);
+        const bool fused = usual(M) && !as_differences;
+        off = fused ? M : m;
         token = (int)tok;
         kind = tok >= V ? 3 : ln_s == INFINITY ? 2 : fused ? 0 : 1;
     }
@@ -263,7 +270,7 @@ __device__ __forceinline__ float error_of(float c, float scale) { return (fmaf(-
 // over thousands of tokens keep.  So would be that ex2's results are 5.0e-8 of themselves too small on the average, alike for all fractions (measured over 4
 // million arguments; 1.4e-7 at most): all terms' but the largest one's, 1 of the sum s.
 __device__ __forceinline__ float logp_of(float xt, float m, float ls, float mean, float s, float scale, float c) {
-    const float off = usual(m) ? kLn2 * (fmaf(m, c, -__fmul_rn(m, c)) + error_of(c, scale) * mean) - 5e-8f * (1.f - 1.f / s) : 0.f;
+    const float M = __fmul_rn(m, c), off = usual(M) ? kLn2 * (fmaf(m, c, -M) + error_of(c, scale) * mean) - 5e-8f * (1.f - 1.f / s) : 0.f;
     return scale * (xt - m) - (ls - off);
 }
 
@@ -573,8 +580,9 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
             Acc acc;
             acc.clear();
             acc.m = warp_max(top);
-            if (usual(acc.m) && row.low > -kHuge) {
-                const F2 cc = f2(c, c), off = f2(-__fmul_rn(acc.m, c), -__fmul_rn(acc.m, c));
+            const float M = __fmul_rn(acc.m, c);
+            if (usual(M) && row.low > -kHuge) {
+                const F2 cc = f2(c, c), off = f2(-M, -M);
 #pragma unroll 4
                 for (i = 0; i < n; i += THREADS) {
                     float f[N];

@@ -593,3 +593,36 @@ def test_the_longest_vocabulary(tk):
     tk.logp_backward(x, tokens, o.norm, torch.ones(1, device="cuda"), out=got)
     assert got[0, -1] == 1.0 and abs(got[0, 0].item() * V + 1.0) < 2.0 ** -8 and (got[0, :-1] == got[0, 0]).all()
     assert (flat[:3] == 7).all() and (flat[3 + V:] == 7).all()
+
+
+def check_fused(tk, x, tokens, scale, g):
+    """The clipped loss without an old policy (the ratio is one): its gradient is that of given gradients of log p and entropy."""
+    R, V = x.shape
+    adv = torch.randn(R, generator=g, device="cuda")
+    got = tk.policy_grad(tk.policy_objective(entropy_coef=0.01, mean="fixed", divisor=float(R)), x, tokens, None, adv, scale=scale)
+    l, H, _, _ = plain.logp(x, tokens, scale)
+    near(got.logp, l, tol_logp(V, l))
+    near(got.entropy, H, rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
+    dl, dh = -adv.double() / R, torch.full((R,), -0.01 / R, dtype=torch.float64, device="cuda")
+    want = plain.dlogits(x, tokens, dl, dh, scale)
+    size = scale * (dl.abs() + dh.abs() * (2 + math.log(V)))[:, None]
+    near(got.dlogits, want, half(x.dtype) * want.abs() + tiny(x.dtype) + (2.0 ** -20 + rel_of(V)) * size)
+    return got
+
+
+@pytest.mark.parametrize("far", [-1e4, -1e9, -1e10, -1e12, -1e15, -1e20, -1e26, 1e6, 1e10])
+@pytest.mark.parametrize("R", [14, 161])
+@pytest.mark.parametrize("V", [4, 100, 200, 1000, 9000, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_finite_masks_and_common_parts(tk, V, dtype, R, far):
+    """Numbers as masks are added with, whole chunks of a row, and rows of nothing else: the largest logit times c has a rounding error of
+    any size, which no exponential may see."""
+    x, tokens, g = make(R, V, DT[dtype], V)
+    x[0::7, : V // 2] += far
+    x[1::7, V // 3:] += far
+    x[2::7, torch.rand(V, generator=g, device="cuda") < 0.5] += far
+    x[3::7] = far
+    x[4::7] += far
+    x[5::7, :-1] = far
+    check_rows(tk, x, tokens, g=g)
+    check_fused(tk, x, tokens, 1.0, g)
