@@ -268,9 +268,10 @@ __device__ __forceinline__ float error_of(float c, float scale) { return (fmaf(-
 // The token's difference to the maximum as it is, less ln of the sum.  That sum is of 2^(x c - M) = e^(scale (x - m)) 2^((m c - M) + error (x - m) c): what M's and
 // c's roundings make of it is taken out to the first order (`mean`: of x c - M under the softmax), or it would be a bias of 1e-8 |l| in every row, which sums
 // over thousands of tokens keep.  So would be that ex2's results are 5.0e-8 of themselves too small on the average, alike for all fractions (measured over 4
-// million arguments; 1.4e-7 at most): all terms' but the largest one's, 1 of the sum s.
+// million arguments; 1.4e-7 at most): all terms' but the largest one's, whose share of the sum s is 2^(m c - M) / s.  (Terms that are differences: M = m c.)
 __device__ __forceinline__ float logp_of(float xt, float m, float ls, float mean, float s, float scale, float c) {
-    const float M = __fmul_rn(m, c), off = usual(M) ? kLn2 * (fmaf(m, c, -M) + error_of(c, scale) * mean) - 5e-8f * (1.f - 1.f / s) : 0.f;
+    const float M = __fmul_rn(m, c), more = usual(M) ? fmaf(m, c, -M) : 0.f, others = 1.f - ex2(more) / s;
+    const float off = kLn2 * (more + error_of(c, scale) * mean) - 5e-8f * (others < 0.f ? 0.f : others);
     return scale * (xt - m) - (ls - off);
 }
 

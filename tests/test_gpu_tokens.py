@@ -626,3 +626,16 @@ def test_finite_masks_and_common_parts(tk, V, dtype, R, far):
     x[5::7, :-1] = far
     check_rows(tk, x, tokens, g=g)
     check_fused(tk, x, tokens, 1.0, g)
+
+
+@pytest.mark.parametrize("scale", [0.7, 1e4, 1e6, 3e7, 1e8, 2.0 ** 40])
+@pytest.mark.parametrize("V", [4, 100, 200, 1000, 9000, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ordinary_logits_at_any_scale(tk, V, dtype, scale):
+    """Not divided by it: the largest logit times c is as large as the scale is.  Half of the rows took their likeliest token; some
+    have a large part in common."""
+    x, tokens, g = make(150, V, DT[dtype], V + 1)
+    x[::3] -= 1e9
+    tokens[::2] = x[::2].float().argmax(1)
+    check_rows(tk, x, tokens, scale, g=g)
+    check_fused(tk, x, tokens, scale, g)
