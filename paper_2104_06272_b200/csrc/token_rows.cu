@@ -272,7 +272,13 @@ __device__ __forceinline__ float error_of(float c, float scale) { return (fmaf(-
 __device__ __forceinline__ float logp_of(float xt, float m, float ls, float mean, float s, float scale, float c) {
     const float M = __fmul_rn(m, c), more = usual(M) ? fmaf(m, c, -M) : 0.f, others = 1.f - ex2(more) / s;
     const float off = kLn2 * (more + error_of(c, scale) * mean) - 5e-8f * (others < 0.f ? 0.f : others);
-    return scale * (xt - m) - (ls - off);
+    const float l = scale * (xt - m) - (ls - off);
+    return l > 0.f ? 0.f : l;  // (the sum's roundings: up to 1e-7 where the token has all the probability; NaN stays)
+}
+// The entropy from ln s and the mean of d (log to base 2); a difference of two equal numbers where one token has all the probability.
+__device__ __forceinline__ float entropy_of(float ls, float mean) {
+    const float H = ls - kLn2 * mean;
+    return H < 0.f ? 0.f : H;
 }
 
 // The elements of a row that lie before the first 16-byte boundary.
@@ -391,7 +397,7 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                 }
                 none = v.s == 0.f;  // a row of -inf alone
                 ls = none ? INFINITY : logf(v.s);
-                H = none ? 0.f : ls - kLn2 * (v.t / v.s);
+                H = none ? 0.f : entropy_of(ls, v.t / v.s);
             }
             float g = 0.f, h = 0.f;
             if (lane == 0 && there) {
@@ -754,7 +760,7 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
                 t = warp_sum(t);
                 const bool none = s == 0.f;  // a row of -inf alone
                 ls = none ? INFINITY : logf(s);
-                H = none ? 0.f : ls - kLn2 * (t / s);
+                H = none ? 0.f : entropy_of(ls, t / s);
                 l = token >= V || !ok ? NAN : none ? -INFINITY : logp_of(xt, m, ls, t / s, s, q.scale, c);
                 if (none) m = 0.f;
                 if (MODE == FUSED && info >= 0) {

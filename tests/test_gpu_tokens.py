@@ -607,6 +607,7 @@ def check_fused(tk, x, tokens, scale, g):
     want = plain.dlogits(x, tokens, dl, dh, scale)
     size = scale * (dl.abs() + dh.abs() * (2 + math.log(V)))[:, None]
     near(got.dlogits, want, half(x.dtype) * want.abs() + tiny(x.dtype) + (2.0 ** -20 + rel_of(V)) * size)
+    assert (got.logp <= 0).all() and (got.entropy >= 0).all()
     return got
 
 
@@ -639,3 +640,17 @@ def test_ordinary_logits_at_any_scale(tk, V, dtype, scale):
     tokens[::2] = x[::2].float().argmax(1)
     check_rows(tk, x, tokens, scale, g=g)
     check_fused(tk, x, tokens, scale, g)
+
+
+@pytest.mark.parametrize("R", [1, 200, 700])
+@pytest.mark.parametrize("V", [5, 100, 129, 500, 2000, 9000, 40000, 131072])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_no_probability_above_one(tk, V, dtype, R):
+    """Rows whose token has nearly all the probability (exp(3.1) V is about the sum of the others): log p is at most 0 and the entropy at least 0."""
+    x, tokens, g = make(R, V, DT[dtype], V + R)
+    x[torch.arange(R, device="cuda"), tokens] = (math.log(V) + 3.1 + torch.linspace(2.0, 25.0, R, device="cuda")).to(x.dtype)
+    l, H, _, _ = plain.logp(x, tokens)
+    for o in (tk.logp(x, tokens), tk.policy_grad(tk.policy_objective(), x, tokens, None, torch.ones(R, device="cuda"))):
+        near(o.logp, l, tol_logp(V, l))
+        near(o.entropy, H, rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
+        assert (o.logp <= 0).all() and (o.entropy >= 0).all()
