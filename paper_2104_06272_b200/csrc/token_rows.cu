@@ -5,8 +5,9 @@
 //   s = sum 2^d,  t = sum 2^d d   in one pass, rescaled whenever m grows;   log p_j = ln2 d_j - ln s;   H = ln s - ln2 t / s
 //   dx_j = scale ( g ([j = token] - p_j) - h p_j (log p_j + H) ) = 2^d_j ( a + b d_j ) + [j = token] scale g
 // M's rounding is the same in every term and cancels while it is small: up to |M| = 2^22 it is 1/8 at most, and the largest term between 2^-1/8 and
-// 2^1/8.  Beyond that (a part of a row where nothing but masks stands, a large scale) it would be an exponent of any size: there d_j = c (x_j - m).  Terms that are -inf give 2^d = 0, and 0 times d is kept from being NaN by a lower bound on d, in those
-// groups of logits only that hold such a term.
+// 2^1/8.  Beyond that (a part of a row where nothing but masks stands, a large scale) it would be an exponent of any size: there d_j = c (x_j - m).
+// Terms that are -inf give 2^d = 0, and 0 times d is kept from being NaN by a lower bound on d, in those groups of logits only that hold such a
+// term, or one far below the others.
 //
 // What bounds these kernels is memory or, in 16-bit types, the issue slots: an element costs an exponential and some 4 other instructions forward
 // and 5 backward, with fused multiply-adds on two floats at a time and maxima on two 16-bit numbers at a time.
@@ -77,7 +78,10 @@ template <class T, int U> __device__ __forceinline__ void extremes(const uint4 (
     }
 }
 
-constexpr float kHuge = 1.2089258e24f;  // 2^80: times c (scale is at most 2^40) far from fp32's largest
+// Exponents from -2^60 on may be multiplied by anything that a gradient has (scale is at most 2^40); where a group's smallest is below, all are bounded by
+// -1000, whose exponential is 0, too.
+__device__ __forceinline__ bool near(float low, float c) { return low * c > -1.1529215e18f; }
+__device__ __forceinline__ F2 floored(F2 d) { return f2(fmaxf(d.x, -1000.f), fmaxf(d.y, -1000.f)); }  // (a NaN comes through its exponential)
 // Terms are relative to M = c m rounded, not to m itself.
 __device__ __forceinline__ bool usual(float M) { return fabsf(M) < 4194304.f; }
 
@@ -141,13 +145,13 @@ struct Acc {
     template <bool BOUND> __device__ __forceinline__ void term(F2 d) {
         const F2 e = f2(ex2(d.x), ex2(d.y));
         s = add2(s, e);
-        t = fma2(e, BOUND ? f2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)) : d, t);  // (a NaN comes through s)
+        t = fma2(e, BOUND ? floored(d) : d, t);
     }
     template <int N> __device__ __forceinline__ void add(const float (&f)[N], float low, float c) {
         const float M = __fmul_rn(m, c);
         if (usual(M)) {
             const F2 cc = f2(c, c), off = f2(-M, -M);
-            if (low > -kHuge) {
+            if (near(low, c)) {
 #pragma unroll
                 for (int k = 0; k < N; k += 2) term<false>(fma2(f2(f[k], f[k + 1]), cc, off));
             } else {
@@ -213,11 +217,11 @@ struct RowGrad {
         const F2 cc = f2(c, c), oo = f2(-off, -off), aa = f2(a, a), bb = f2(b, b);
         auto one = [&](int k, F2 d, bool bound) {
             const F2 e = f2(ex2(d.x), ex2(d.y));
-            const F2 y = mul2(e, fma2(bb, bound ? f2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)) : d, aa));
+            const F2 y = mul2(e, fma2(bb, bound ? floored(d) : d, aa));
             f[k] = y.x;
             f[k + 1] = y.y;
         };
-        if (kind == 0 && low > -kHuge) {
+        if (kind == 0 && near(low, c)) {
 #pragma unroll
             for (int k = 0; k < N; k += 2) one(k, fma2(f2(f[k], f[k + 1]), cc, oo), false);
         } else if (kind == 0) {
@@ -588,7 +592,7 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
             acc.clear();
             acc.m = warp_max(top);
             const float M = __fmul_rn(acc.m, c);
-            if (usual(M) && row.low > -kHuge) {
+            if (usual(M) && near(row.low, c)) {
                 const F2 cc = f2(c, c), off = f2(-M, -M);
 #pragma unroll 4
                 for (i = 0; i < n; i += THREADS) {
@@ -668,7 +672,7 @@ __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideAr
                 T* part_out = out + now.head + (size_t)begin * N;
                 const int j0 = now.head + begin * N;
                 const bool vec = ((uintptr_t)part_out & 15) == 0;
-                const bool fast = g.kind == 0 && row.low > -kHuge && vec;
+                const bool fast = g.kind == 0 && near(row.low, c) && vec;
                 if (fast) {
                     const F2 cc = f2(c, c), oo = f2(-g.off, -g.off), aa = f2(g.a, g.a), bb = f2(g.b, g.b);
                     const int at = g.token - j0;  // the taken token, from this thread's first element on

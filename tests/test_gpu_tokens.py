@@ -654,3 +654,26 @@ def test_no_probability_above_one(tk, V, dtype, R):
         near(o.logp, l, tol_logp(V, l))
         near(o.entropy, H, rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
         assert (o.logp <= 0).all() and (o.entropy >= 0).all()
+
+
+@pytest.mark.parametrize("scale", [1.0, 1e9, 2.0 ** 40])
+@pytest.mark.parametrize("V", [4, 100, 200, 1000, 9000, 40000])
+def test_gradients_of_entropies_at_any_scale(tk, V, scale):
+    """Scaled logits of ordinary size beside tokens without probability: -inf, the lowest value, and what lies between."""
+    x, tokens, g = make(161, V, torch.float32, V + 2)
+    x /= scale
+    for i, low in enumerate((-math.inf, torch.finfo(torch.float32).min, -1e15, -1e22)):
+        x[i::5, torch.rand(V, generator=g, device="cuda") < 0.5] = low
+    x[:, 0] = 1.0 / scale
+    o = tk.logp(x, tokens, scale=scale)
+    l, H, _, _ = plain.logp(x, tokens, scale)
+    near(o.logp, l.float(), tol_logp(V, l))  # (-1e47 is -inf in 32 bits)
+    near(o.entropy, H, rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
+    dl, dh = torch.randn(161, generator=g, device="cuda"), torch.randn(161, generator=g, device="cuda")
+    got = tk.logp_backward(x, tokens, o.norm, dl, entropy=o.entropy, dentropy=dh, scale=scale)
+    want = plain.dlogits(x, tokens, dl, dh, scale)
+    near(got, want, rel_of(V) * scale * (dl.abs() + dh.abs() * (2 + math.log(V))).double()[:, None])
+    adv = torch.randn(161, generator=g, device="cuda")
+    both = tk.policy_grad(tk.policy_objective(entropy_coef=0.3, mean="fixed"), x, tokens, None, adv, scale=scale)
+    want = plain.dlogits(x, tokens, -adv, torch.full_like(adv, -0.3), scale)
+    near(both.dlogits, want, (2.0 ** -20 + rel_of(V)) * scale * (adv.abs() + 0.3 * (2 + math.log(V))).double()[:, None])
