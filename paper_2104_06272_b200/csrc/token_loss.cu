@@ -318,7 +318,7 @@ __device__ __forceinline__ void pair_terms(const PreferArgs& A, double z, double
     if (A.kind == ANAKIN_PREFER_SIGMOID) {
         const double e = (double)A.smoothing;
         loss = (1.0 - e) * softplus(-z) + e * softplus(z);
-        dz = 1.0 / (1.0 + exp(-z)) - (1.0 - e);
+        dz = e - 1.0 / (1.0 + exp(z));  // (not sigmoid(z) - (1 - e), which loses the digits of a slope near 0)
     } else if (A.kind == ANAKIN_PREFER_HINGE) {
         loss = z < 1.0 ? 1.0 - z : z >= 1.0 ? 0.0 : z;
         dz = z >= 1.0 ? 0.0 : -1.0;

@@ -677,3 +677,13 @@ def test_gradients_of_entropies_at_any_scale(tk, V, scale):
     both = tk.policy_grad(tk.policy_objective(entropy_coef=0.3, mean="fixed"), x, tokens, None, adv, scale=scale)
     want = plain.dlogits(x, tokens, -adv, torch.full_like(adv, -0.3), scale)
     near(both.dlogits, want, (2.0 ** -20 + rel_of(V)) * scale * (adv.abs() + 0.3 * (2 + math.log(V))).double()[:, None])
+
+
+@pytest.mark.parametrize("z", [5.0, 20.0, 30.0, 38.0, 60.0, 85.0, -85.0])
+def test_preference_gradients_of_decided_pairs(tk, z):
+    """The sigmoid's slope keeps its digits where it is small: terms in 64 bits, rounded once."""
+    l = torch.tensor([z, 0.0], device="cuda")
+    off = torch.tensor([0, 1, 2], device="cuda")
+    o = tk.preference_loss(tk.preference_objective("sigmoid", beta=1.0), l, off)
+    want = -1.0 / (1.0 + math.exp(z))
+    assert abs(o.dlogp[0].item() - want) <= 2.0 ** -23 * abs(want) and o.dlogp[1].item() == -o.dlogp[0].item()
