@@ -29,50 +29,68 @@ struct Args {
     bool vec_x, vec_y;  // every row starts on a 16-byte boundary
 };
 
-// 1 / (1 + exp(-x)): 0 for x below -126 ln2 (there x times it is below 2^-119), NaN stays.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + tok::ex2(-tok::kLog2e * x)); }
-// The normal distribution function and its density (times sqrt(2 pi)) of two numbers: 1 - Q(|x|) and the like with Hastings' rational approximation of
-// erfc (Abramowitz and Stegun 7.1.26: off by at most 1.5e-7), which needs the density's exponential and no branch.
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-__device__ __forceinline__ float2 normal(float2 x, float2& density) {
-    const float2 z = __fmul2_rn(make_float2(fabsf(x.x), fabsf(x.y)), both(0.70710678118654752f));
-    const float2 e = __fmul2_rn(__fmul2_rn(z, z), both(-tok::kLog2e)), u = __ffma2_rn(z, both(0.3275911f), both(1.f));
-    density = make_float2(tok::ex2(e.x), tok::ex2(e.y));
+__device__ __forceinline__ float2 ex2(float2 v) { return make_float2(tok::ex2(v.x), tok::ex2(v.y)); }
+// FINE (fp32): what a product's rounding r takes from an exponent is put back, 2^(q + r) = 2^q (1 + r ln 2); r is below 2^-16.  16-bit types do not see it.
+constexpr float kLog2eRest = 1.925963e-8f;  // log2(e) is kLog2e + this
+__device__ __forceinline__ float2 put_back(float2 e, float2 r) { return __ffma2_rn(__fmul2_rn(e, both(tok::kLn2)), r, e); }
+
+// 1 / (1 + exp(-x)): 0 for x below -126 ln2 (there x times it is below 2^-119), NaN stays, but not in FINE (x times it is one all the same).
+template <bool FINE> __device__ __forceinline__ float2 sigmoid(float2 x) {
+    float2 e;
+    if (FINE) {  // (exp(88) has an fp32 number, and 1 / (1 + it) is given as 0)
+        const float2 a = make_float2(fminf(fmaxf(-x.x, -200.f), 88.f), fminf(fmaxf(-x.y, -200.f), 88.f)), q = __fmul2_rn(a, both(tok::kLog2e));
+        e = put_back(ex2(q), __ffma2_rn(a, both(kLog2eRest), __ffma2_rn(a, both(tok::kLog2e), make_float2(-q.x, -q.y))));
+    } else {
+        e = ex2(__fmul2_rn(x, both(-tok::kLog2e)));
+    }
+    return make_float2(__fdividef(1.f, 1.f + e.x), __fdividef(1.f, 1.f + e.y));
+}
+// The normal distribution function and its density (times sqrt(2 pi)) of two numbers.  Q(|x|) = exp(-x^2 / 2) times a polynomial in t = 1 / (1 + p |x|) without a
+// constant term, fitted for this file (least squares, reweighted until the largest error is smallest, over 0 <= |x| <= 16): nine terms, off by 1.6e-8 of Q
+// (evaluated in fp32 4e-7); for 16-bit types six, off by 7e-8 or, where Q is below 1e-3, 7e-5 of it.
+template <bool FINE> __device__ __forceinline__ float2 normal(float2 x, float2& density) {
+    constexpr float kFine[9] = {0.106401980f, 0.106038909f, 0.102237833f, 0.0648655083f, 0.126530668f, -0.0988459486f, 0.200554947f, -0.137941195f, 0.0301573012f};
+    constexpr float kShort[6] = {0.117681872f, 0.106051226f, 0.164907422f, -0.0652277831f, 0.261766630f, -0.0851794475f};
+    constexpr float kHalfLog2e = -0.5f * tok::kLog2e;
+    float2 z = make_float2(fabsf(x.x), fabsf(x.y)), p;
+    if (FINE) {  // (from 16 on the density is 0)
+        z = make_float2(fminf(z.x, 16.f), fminf(z.y, 16.f));
+        const float2 h = __fmul2_rn(z, z), l = __ffma2_rn(z, z, make_float2(-h.x, -h.y)), q = __fmul2_rn(h, both(kHalfLog2e));
+        const float2 r = __ffma2_rn(h, both(kHalfLog2e), make_float2(-q.x, -q.y));
+        density = put_back(ex2(q), __ffma2_rn(l, both(kHalfLog2e), __ffma2_rn(h, both(-0.5f * kLog2eRest), r)));
+    } else {
+        density = ex2(__fmul2_rn(__fmul2_rn(z, z), both(kHalfLog2e)));
+    }
+    const float2 u = __ffma2_rn(z, both(FINE ? 0.266672194f : 0.293045700f), both(1.f));
     const float2 t = make_float2(__fdividef(1.f, u.x), __fdividef(1.f, u.y));
-    float2 p = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
-    p = __ffma2_rn(t, p, both(0.5f * 1.421413741f));
-    p = __ffma2_rn(t, p, both(0.5f * -0.284496736f));
-    p = __ffma2_rn(t, p, both(0.5f * 0.254829592f));
+    constexpr int N = FINE ? 9 : 6;
+    p = both(FINE ? kFine[8] : kShort[5]);
+#pragma unroll
+    for (int k = N - 2; k >= 0; --k) p = __ffma2_rn(t, p, both(FINE ? kFine[k] : kShort[k < 6 ? k : 5]));
     const float2 q = __fmul2_rn(__fmul2_rn(density, t), p);
     return make_float2(x.x > 0.f ? 1.f - q.x : q.x, x.y > 0.f ? 1.f - q.y : q.y);
 }
-template <int ACT> __device__ __forceinline__ float2 act_of(float2 x) {
-    auto one = [](float v) {
-        if (ACT == ANAKIN_ACT_RELU) return v > 0.f ? v : v != v ? v : 0.f;
-        if (ACT == ANAKIN_ACT_SILU) return v == -INFINITY ? 0.f : v * sigmoid(v);
-        return v;
-    };
-    if (ACT == ANAKIN_ACT_GELU) {
+template <bool FINE, int ACT> __device__ __forceinline__ float2 act_of(float2 x) {
+    if (ACT == ANAKIN_ACT_SILU || ACT == ANAKIN_ACT_GELU) {
         float2 d;
-        const float2 y = __fmul2_rn(x, normal(x, d));
+        const float2 y = __fmul2_rn(x, ACT == ANAKIN_ACT_SILU ? sigmoid<FINE>(x) : normal<FINE>(x, d));
         return make_float2(x.x == -INFINITY ? 0.f : y.x, x.y == -INFINITY ? 0.f : y.y);
     }
+    auto one = [](float v) { return ACT == ANAKIN_ACT_RELU ? (v > 0.f ? v : v != v ? v : 0.f) : v; };
     return make_float2(one(x.x), one(x.y));
 }
-template <int ACT> __device__ __forceinline__ float2 slope_of(float2 x) {
-    auto one = [](float v) {
-        if (ACT == ANAKIN_ACT_RELU) return v > 0.f ? 1.f : v != v ? v : 0.f;
-        if (ACT == ANAKIN_ACT_SILU) {
-            const float g = sigmoid(v);
-            return fmaf(v * g, 1.f - g, g);
-        }
-        return 1.f;
-    };
+template <bool FINE, int ACT> __device__ __forceinline__ float2 slope_of(float2 x) {
+    if (ACT == ANAKIN_ACT_SILU) {
+        const float2 g = sigmoid<FINE>(x);
+        return __ffma2_rn(__fmul2_rn(x, g), make_float2(1.f - g.x, 1.f - g.y), g);
+    }
     if (ACT == ANAKIN_ACT_GELU) {
         float2 d;
-        const float2 n = normal(x, d);
+        const float2 n = normal<FINE>(x, d);
         return __ffma2_rn(__fmul2_rn(x, both(0.39894228040143268f)), d, n);
     }
+    auto one = [](float v) { return ACT == ANAKIN_ACT_RELU ? (v > 0.f ? 1.f : v != v ? v : 0.f) : 1.f; };
     return make_float2(one(x.x), one(x.y));
 }
 
@@ -239,7 +257,7 @@ __global__ void __launch_bounds__(256) k_ckpt_forward(Args a) {
                     float g[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
-                        const float2 v = act_of<ACT>(make_float2(f[i], f[i + 1]));
+                        const float2 v = act_of<sizeof(T) == 4, ACT>(make_float2(f[i], f[i + 1]));
                         g[i] = v.x;
                         g[i + 1] = v.y;
                     }
@@ -284,7 +302,7 @@ __global__ void __launch_bounds__(256) k_ckpt_read(Args a) {
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 if (BACK) {
-                    const float2 g = __fmul2_rn(make_float2(f[i], f[i + 1]), slope_of<ACT>(make_float2(v[i], v[i + 1])));
+                    const float2 g = __fmul2_rn(make_float2(f[i], f[i + 1]), slope_of<sizeof(T) == 4, ACT>(make_float2(v[i], v[i + 1])));
                     v[i] = g.x;
                     v[i + 1] = g.y;
                 } else {

@@ -293,3 +293,24 @@ def test_refusals_of_tensors(tk):
         assert e.value.code == -4
     again = tk.ckpt_forward(x)
     assert torch.equal(again[0], y) and torch.equal(again[1].codes, q) and torch.equal(again[1].scales, s)
+
+
+@pytest.mark.parametrize("act,lo,hi", [("silu", -100.0, -3.0), ("gelu", -14.0, -2.0)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_tails_of_the_activations(tk, dtype, act, lo, hi):
+    """Where they are near 0, against their own size.  fp32: the exponential's 2^-22, the quotient's 2 ulp, polynomial and products: 1.1 2^-20 of the value,
+    2^-19 is allowed; the slopes' two terms cancel by a factor below 2 there.  16-bit types: the fit's 7e-5 and the exponent's rounding, 2^-13 is allowed beside
+    the type's own half step.  Exponentials below 2^-126 are 0."""
+    dt = DT[dtype]
+    x = torch.linspace(lo, hi, 96 * 64, device="cuda").view(96, 64).to(dt)
+    rel = 2.0 ** -19 if dtype == "f32" else half(dt) + 2.0 ** -13
+    least = 2.0 ** -118 if dtype != "f16" else torch.finfo(dt).smallest_normal * torch.finfo(dt).eps
+    y, ck = tk.ckpt_forward(x, act)
+    below = lambda v: 0.5 * torch.erfc(-v / math.sqrt(2.0))  # noqa: E731  (the normal distribution function; 1 + erf would lose it here)
+    v = x.double()
+    want = v * torch.sigmoid(v) if act == "silu" else v * below(v)
+    near(y, want, rel * want.abs() + least)
+    v = plain.kept(x)[0]
+    dx = tk.ckpt_backward(ck, torch.ones_like(x), act)
+    want = plain.slope(act, v) if act == "silu" else below(v) + v * torch.exp(-v * v / 2) / math.sqrt(2.0 * math.pi)
+    near(dx, want, rel * want.abs() + least)
