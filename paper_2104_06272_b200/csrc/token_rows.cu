@@ -304,15 +304,18 @@ template <class T> __device__ __forceinline__ void store_vector(T* out, const ui
     }
 }
 
-// A group of G threads works on one row: G <= 32 lanes of a warp, or the whole block.  Rows are read straight into registers; where the gradient
-// follows (FUSED, rows of up to 1 KB) the second reading comes from the caches.  A thread alone takes a row element by element.
+// A group of G threads works on one row: G <= 32 lanes of a warp, or the whole block (of 256 threads, or 1024).  Rows are read straight into registers; where the gradient
+// follows (FUSED, rows of up to 1 KB, and those that no cluster holds) the second reading comes from the caches where the row fits.  A thread alone takes a row element by element.
 // Backward alone, few rows: gridDim.y blocks share a row.
+constexpr int threads_of(int G) { return G > 256 ? G : 256; }
 template <class T, int G, int MODE>
-__global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
+__global__ void __launch_bounds__(threads_of(G)) k_token_rows(RowArgs A) {
     pdl_wait();
-    __shared__ float4 red[2][8];
-    __shared__ double redd[8 * kPolicyParts];
-    constexpr int GROUPS = 256 / G, N = Vec<T>::N, U = 4;
+    constexpr int WARPS = threads_of(G) / 32;
+    __shared__ float4 red[2][WARPS];
+    __shared__ double redd[WARPS * kPolicyParts];
+    __shared__ float2 both;  // of the row that the block works on (it is written again behind the barrier of the next row's sums)
+    constexpr int GROUPS = threads_of(G) / G, N = Vec<T>::N, U = 4;
     const Rows& q = A.q;
     const int lane = threadIdx.x % G, V = (int)q.vocab;
     const float c = q.scale * kLog2e;
@@ -394,10 +397,10 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                     // (two sets: a warp may be a row ahead of one that still reads)
                     if ((threadIdx.x & 31) == 0) red[flip][threadIdx.x >> 5] = make_float4(v.m, v.s, v.t, 0.f);
                     __syncthreads();
-                    const float4 p = red[flip][threadIdx.x & 7];
+                    const float4 p = red[flip][threadIdx.x % WARPS];
                     flip ^= 1;
                     v = Soft{p.x, p.y, p.z};
-                    group_sum<8>(v, c);
+                    group_sum<WARPS>(v, c);
                 }
                 none = v.s == 0.f;  // a row of -inf alone
                 ls = none ? INFINITY : logf(v.s);
@@ -422,10 +425,16 @@ __global__ void __launch_bounds__(256) k_token_rows(RowArgs A) {
                 }
             }
             if constexpr (MODE == FUSED) {
-                static_assert(G <= 32, "rows of whole blocks are k_token_rows_wide's");
-                const int src = (threadIdx.x & 31) / G * G;
-                g = __shfl_sync(0xFFFFFFFFu, g, src);
-                h = __shfl_sync(0xFFFFFFFFu, h, src);
+                if constexpr (G > 32) {  // (the token's logit has been read before anything is stored, in place, too)
+                    if (lane == 0) both = make_float2(g, h);
+                    __syncthreads();
+                    g = both.x;
+                    h = both.y;
+                } else {
+                    const int src = (threadIdx.x & 31) / G * G;
+                    g = __shfl_sync(0xFFFFFFFFu, g, src);
+                    h = __shfl_sync(0xFFFFFFFFu, h, src);
+                }
                 gr.set(v.m, ls, g, h, H, q.scale, c, token, V, as_differences);
             }
         } else if (counts) {
@@ -873,7 +882,7 @@ cudaError_t launch_wide(const WideArgs& W, int* parts, cudaStream_t s) {
 
 template <class T, int G, int MODE>
 cudaError_t launch_rows(const RowArgs& A, int* parts, cudaStream_t s) {
-    constexpr int GROUPS = 256 / G;
+    constexpr int GROUPS = threads_of(G) / G;
     const long long ctas = (A.q.rows + GROUPS - 1) / GROUPS;
     const int grid = (int)(ctas < kMaxPartials ? ctas : kMaxPartials);
     int share = 1;  // blocks of a row
@@ -882,7 +891,7 @@ cudaError_t launch_rows(const RowArgs& A, int* parts, cudaStream_t s) {
         while (share < 16 && grid * share < 148 * 4 && vecs > 512ll * share) share *= 2;
     }
     if (parts) *parts = grid;
-    return launch<k_token_rows<T, G, MODE>>(dim3(grid, share), dim3(256), 0, s, A);
+    return launch<k_token_rows<T, G, MODE>>(dim3(grid, share), dim3(threads_of(G)), 0, s, A);
 }
 
 template <class T, int MODE>
@@ -902,9 +911,13 @@ cudaError_t launch_rows_t(const RowArgs& A, int* parts, cudaStream_t s) {
     }
     // a warp a row while that gives every SM its fill of rows, several times over where rows are long (forward: 32768 x 12000 bf16 153 us, by whole
     // blocks 291; backward by blocks 260, by warps 281)
-    if (MODE == FUSED || bytes <= 4096 || (bytes <= 16384 && A.q.rows >= 148 * 16) || (MODE == FORWARD && bytes <= 65536 && A.q.rows >= 148 * 192)) return launch_rows<T, 32, MODE>(A, parts, s);
-    if constexpr (MODE != FUSED) return launch_rows<T, 256, MODE>(A, parts, s);
-    return cudaErrorNotSupported;
+    if constexpr (MODE == FUSED) {
+        // rows that no cluster holds, above 872 KB (64 x 262144 fp32: 59 us by blocks of 1024 threads, by those of 256 159, by warps 1004)
+        return launch_rows<T, 1024, MODE>(A, parts, s);
+    } else {
+        if (bytes <= 4096 || (bytes <= 16384 && A.q.rows >= 148 * 16) || (MODE == FORWARD && bytes <= 65536 && A.q.rows >= 148 * 192)) return launch_rows<T, 32, MODE>(A, parts, s);
+        return launch_rows<T, 256, MODE>(A, parts, s);
+    }
 }
 
 template <int MODE>

@@ -687,3 +687,16 @@ def test_preference_gradients_of_decided_pairs(tk, z):
     o = tk.preference_loss(tk.preference_objective("sigmoid", beta=1.0), l, off)
     want = -1.0 / (1.0 + math.exp(z))
     assert abs(o.dlogp[0].item() - want) <= 2.0 ** -23 * abs(want) and o.dlogp[1].item() == -o.dlogp[0].item()
+
+
+@pytest.mark.parametrize("R,V,dtype", [(3, 262144, "f32"), (70, 230001, "f32"), (5, 500001, "bf16"), (700, 223300, "f32")])
+def test_policy_grad_of_rows_that_no_cluster_holds(tk, R, V, dtype):
+    x, tokens, g = make(R, V, DT[dtype], R, ignored=0.2 if R > 3 else 0.0)
+    got = check_fused(tk, x, tokens, 0.9, g)
+    again = tk.policy_grad(tk.policy_objective(), x, tokens, None, torch.ones(R, device="cuda"), scale=0.9)
+    assert torch.equal(again.logp, got.logp)
+    obj, adv = tk.policy_objective(entropy_coef=0.1), torch.randn(R, generator=g, device="cuda")
+    a = tk.policy_grad(obj, x, tokens, None, adv)
+    y = x.clone()
+    b = tk.policy_grad(obj, y, tokens, None, adv, out=y)  # in place
+    assert torch.equal(y, a.dlogits) and torch.equal(a.stats, b.stats)
