@@ -1,6 +1,8 @@
 // The losses over tokens from log-probabilities: the clipped policy loss with a KL term, and the preference loss over pairs of answers; and the
 // counts of rows that their means divide by.  All of it is a few vectors of one number a token: the launches cost more than the
 // bytes up to some hundred thousand tokens, so short batches are done by one CTA in one launch.
+#include <algorithm>
+
 #include "token_rows.cuh"
 
 namespace anakin {
@@ -516,7 +518,8 @@ extern "C" {
 
 int anakin_token_workspace_bytes(int64_t rows, int64_t sequences, size_t* bytes) {
     if (!bytes || rows < 0 || sequences < 0 || rows >= (int64_t(1) << 31) || sequences >= (int64_t(1) << 31) - 1) return ANAKIN_E_INVALID_ARG;
-    *bytes = carve(nullptr, rows, sequences < 1 ? 1 : sequences).bytes;
+    // (the one sequence of rows without offsets may be shared by more blocks than a few of them)
+    *bytes = std::max(carve(nullptr, rows, 1).bytes, carve(nullptr, rows, sequences).bytes);
     return ANAKIN_OK;
 }
 

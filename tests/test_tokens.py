@@ -184,3 +184,16 @@ def test_gradients_at_odd_addresses_are_refused(tk):
         r, out = rows_of(tk, dtype=dtype), C.c_void_p(at)
         assert lib.anakin_token_logp_backward(C.byref(r), FAKE, FAKE, FAKE, FAKE, out, 100, None) == -1
         assert lib.anakin_token_policy_grad(C.byref(r), C.byref(obj), FAKE, FAKE, None, FAKE, None, None, out, 100, FAKE, 1 << 30, None) == -1
+
+
+def test_a_workspace_for_sequences_does_for_rows_without_offsets(tk):
+    """Without offsets all rows are one sequence, whatever the number of sequences says: the workspace asked for with that number has room."""
+    lib, n = tk._lib, C.c_size_t(0)
+
+    def size(rows, sequences):
+        assert lib.anakin_token_workspace_bytes(rows, sequences, C.byref(n)) == 0
+        return n.value
+
+    for rows in (1, 1000, 62464, 63000, 127 * 1024, 10 ** 6, (1 << 31) - 1):
+        for sequences in (0, 1, 2, 3, 7, 60, 1000):
+            assert size(rows, sequences) >= size(rows, 1)
