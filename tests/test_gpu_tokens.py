@@ -700,3 +700,33 @@ def test_policy_grad_of_rows_that_no_cluster_holds(tk, R, V, dtype):
     y = x.clone()
     b = tk.policy_grad(obj, y, tokens, None, adv, out=y)  # in place
     assert torch.equal(y, a.dlogits) and torch.equal(a.stats, b.stats)
+
+
+@pytest.mark.parametrize("R,V,dtype", [(14500, 1500, "bf16"), (9100, 5000, "bf16"), (9100, 2500, "f32"), (3500, 15000, "bf16"), (1500, 60000, "bf16"), (1500, 40000, "f32"), (480, 220000, "f16")])
+def test_a_dozen_rows_a_cluster(tk, R, V, dtype):
+    """Rows held on chip, so many that every block or cluster takes a dozen: sets of sums and constants are used again, with rows that do not count
+    between those that do, one at a time and many in a row."""
+    x, tokens, g = make(R, V, DT[dtype], R, ignored=0.3)
+    tokens[R // 3: R // 2] = -100
+    x[tokens < 0] = math.nan
+    S = 9
+    _, _, adv, _, _, offsets, _ = policy_inputs(R, S, g, R // 20)
+    f, obj = objective(tk, mean="sequence", kl="k2")
+    step = max(1, (1 << 26) // V)  # (64-bit forms of a few rows at a time)
+    parts = [plain.logp(x[r: r + step], tokens[r: r + step])[:2] for r in range(0, R, step)]
+    l, H = (torch.cat([p[i] for p in parts]) for i in (0, 1))
+    old = off_the_edge(f, l, (l + 0.2 * torch.randn(R, generator=g, device="cuda")).float())
+    ref = (l + 0.2 * torch.randn(R, generator=g, device="cuda")).float()
+    got = tk.policy_grad(obj, x, tokens, old, adv, ref_logp=ref, offsets=offsets)
+    stats, dl, dh = plain.policy(f, l, old, adv, ref, H, tokens, None, offsets)
+    near(got.logp, l, tol_logp(V, l))
+    near(got.entropy, H, rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
+    near(got.stats, stats, (2.0 ** -19 + 4 * float(tol_logp(V, l).max())) * (2 + float(adv.abs().max()) + math.log(V)))
+    slack = (2.0 ** -20 + 3 * tol_logp(V, l) + rel_of(V)) * (dl.abs() + dh.abs() * (2 + math.log(V)) + dl.abs().max())
+    for r in range(0, R, step):
+        at = slice(r, r + step)
+        want = plain.dlogits(x[at], tokens[at], dl[at], dh[at])
+        near(got.dlogits[at], want, half(x.dtype) * want.abs() + tiny(x.dtype) + slack[at, None])
+    o = tk.logp(x[:590], tokens[:590])  # (so many rows of the longer ones go through clusters in this call, too)
+    near(o.logp, l[:590], tol_logp(V, l[:590]))
+    near(o.entropy, H[:590], rel_of(V) * (1 + math.log(V)) + 2.0 ** -22 * (math.log(V) + 1))
