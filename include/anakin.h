@@ -350,8 +350,10 @@ int anakin_noalloc_status(void* cuda_stream, int* device_status);
  * Rows.  A row of the logits is the distribution of one token; the rows of all sequences lie one after the other.  Row r belongs to the
  * sequence i with offsets[i] <= r < offsets[i+1]; without offsets all rows are one sequence.  A row COUNTS when tokens[r] >= 0 (where
  * tokens are given), mask[r] != 0 (where a mask is given) and, for the losses, it belongs to a sequence.  What a row that does not count holds is
- * never used, NaN included: its outputs are zeros.  A token >= vocab gives NaN.  Logits of -inf are tokens without probability; a row of
- * nothing else has logp -inf, entropy 0 and a gradient of zeros.  NaN or +inf among a row's logits gives NaN.
+ * never used, NaN included: its outputs are zeros.  (anakin_token_logp does not look at offsets, and the logp and entropy of anakin_token_policy_grad are
+ * that call's: a row behind the last sequence has them, but no part in the loss and a gradient of zeros.)  A token >= vocab gives NaN.  Logits of -inf are tokens without probability; a row of
+ * nothing else has logp -inf, entropy 0 and a gradient of zeros; any finite logits, masks of -1e9 or -1e20 among them, are logits.  logp is at most 0
+ * and the entropy at least 0.  NaN or +inf among a row's logits gives NaN.
  * A row that some blocks share waits for their sums, with a limit: should one run out, what follows is NaN.
  * Offsets that do not ascend, or pass [0, rows], are an error of the caller's that the kernels answer with wrong numbers, within bounds.
  */
@@ -419,8 +421,9 @@ typedef struct anakin_preference_objective {
 
 /*
  * Log-probability of every row's token, and the entropy of its distribution.
- *   out  logp f32[rows]; entropy f32[rows] or NULL; norm f32[rows][2] or NULL: the largest logit m and log sum exp(scale (x - m)), which
- *        the gradient needs (the row's log-sum-exp is scale m + the second)
+ *   out  logp f32[rows]; entropy f32[rows] or NULL; norm f32[rows][2] or NULL, which the gradient needs: the largest logit m, and log sum exp(scale x - M)
+ *        with M an fp32 rounding of scale m (or scale m itself, where that is large).  scale m + the second is the row's log-sum-exp but for a rounding
+ *        of its size.
  * No workspace.  Offsets are not looked at.
  */
 int anakin_token_logp(const anakin_token_rows* rows, float* logp, float* entropy, float* norm, void* cuda_stream);
@@ -448,8 +451,8 @@ int anakin_token_policy_loss(const anakin_token_rows* rows, const anakin_policy_
                              void* dev_workspace, size_t bytes, void* cuda_stream);
 
 /*
- * The clipped loss from logits, with the gradient of the logits, in one pass over them: equal to anakin_token_logp,
- * anakin_token_policy_loss and anakin_token_logp_backward in a row.  logp and entropy (f32[rows]) may be NULL.  dlogits as in
+ * The clipped loss from logits, with the gradient of the logits, in one pass over them (two where a row is longer than 872 KB): equal to
+ * anakin_token_logp, anakin_token_policy_loss and anakin_token_logp_backward in a row.  logp and entropy (f32[rows]) may be NULL.  dlogits as in
  * anakin_token_logp_backward.
  */
 int anakin_token_policy_grad(const anakin_token_rows* rows, const anakin_policy_objective* objective, const float* old_logp, const float* adv,
@@ -481,7 +484,8 @@ enum { ANAKIN_ACT_IDENTITY = 0, ANAKIN_ACT_RELU = 1, ANAKIN_ACT_SILU = 2, ANAKIN
 /* Sizes of the two arrays of a checkpoint. */
 int anakin_ckpt_bytes(int64_t rows, int64_t cols, size_t* code_bytes, size_t* scale_bytes);
 
-/* y = act(x) and the checkpoint of x in one pass over x; y (dtype of x) may be NULL, or x itself. */
+/* y = act(x) and the checkpoint of x in one pass over x; y (dtype of x) may be NULL, or x itself.  SiLU and GELU are off by less than 2^-19 of
+ * themselves in fp32, before 16-bit types' rounding by 2^-13 of themselves or 2^-20 of x, whichever is less; exponentials below 2^-126 are 0. */
 int anakin_ckpt_forward(int dtype, int act, int64_t rows, int64_t cols, const void* x, int64_t ldx, void* y, int64_t ldy, uint8_t* codes,
                         uint8_t* scales, void* cuda_stream);
 

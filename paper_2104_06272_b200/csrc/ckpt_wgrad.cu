@@ -17,7 +17,8 @@
 // The chunks of all tiles, one tile after the other, are dealt out in equal runs, so that every SM has the same work; a tile that several runs share is
 // summed from partial tiles, in their order, by a last kernel.
 // What bounds it: shared memory.  A chunk of a lone CTA's 128 x 256 tile moves 112 KB there in the 512 cycles of its MMAs, a pair's 80 KB (dY's half is
-// fetched and read once by each).  524288 x 1024 x 1024 bf16: 975 us, 1.13 PFLOP/s (cuBLAS, the bf16 product alone: 826).
+// fetched and read once by each).  524288 x 1024 x 1024 bf16: 976 us in a burst, 1.13 PFLOP/s, and 1143 sustained
+// (cuBLAS, the bf16 product alone: 816 and 980).  The tensor pipe is active 54 % of the time: codes come late, too.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>

@@ -498,7 +498,7 @@ __device__ __forceinline__ void copies_but(int n) {
 // One warp more joins the sums: every warp's go into the shared memory of all blocks of the cluster (st.async, counted on an mbarrier; a cluster
 // barrier would also wait for the gradient's stores to memory), and while the others work on the next row it takes the token's terms of the
 // loss and leaves the row's constants for them.
-// The logits are read from memory once and their gradient written once.  8192 x 131072 bf16: 873 us, 4.9 TB/s (memory's share of it 654); issue slots and the
+// The logits are read from memory once and their gradient written once.  8192 x 131072 bf16, a tenth without a token: 878 us, 4.6 TB/s (at the copy rate 621); issue slots and the
 // exponentials' unit are two thirds used.
 template <class T, int THREADS, int PER_SM, int MODE>
 __global__ void __launch_bounds__(THREADS + 32, PER_SM) k_token_rows_wide(WideArgs W) {
@@ -823,7 +823,7 @@ WidePlan wide_plan(const Rows& q, size_t es) {
         return p;
     }
     // Two rows' parts a block: 54 KB each with two blocks an SM (three up to 35 KB: 16384 x 32000 bf16 471 us, with two 506), 110 KB with one.  Large
-    // parts, as every row costs every thread some 250 instructions besides its vectors (8192 x 131072 bf16 in clusters of 5 873 us, of 8 948).
+    // parts, as every row costs every thread some 250 instructions besides its vectors (8192 x 131072 bf16 in clusters of 5 878 us, of 8 some 950).
     auto blocks = [&](long long most) { return (int)((vecs * 16 + most - 1) / most); };
     const int b = blocks(54272), d = blocks(111616);
     p.threads = b <= kMaxCluster ? 256 : d <= kMaxCluster ? 512 : 0;

@@ -113,7 +113,8 @@ def _one_of(table: dict, name: str, key: str) -> int:
 
 
 def logp(logits: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, mask: torch.Tensor | None = None, entropy: bool = True) -> TokenLogp:
-    """Log-probability of every row's token under softmax(scale * logits), and the entropy (anakin_token_logp)."""
+    """Log-probability of every row's token under softmax(scale * logits), and the entropy (anakin_token_logp).  No grad_fn, whatever the logits have:
+    logp_backward is the gradient."""
     return TokenLogp._make(_host.logp(logits, tokens, scale, mask, entropy))
 
 
@@ -145,7 +146,8 @@ def preference_loss(objective: PreferenceObjective, logp: torch.Tensor, offsets:
 
 
 def ckpt_forward(x: torch.Tensor, act: str = "relu", y: bool = True, out: torch.Tensor | None = None) -> tuple[torch.Tensor | None, Checkpoint]:
-    """act(x) (None with y=False) and the checkpoint of x in 8 bits (anakin_ckpt_forward); `out` may be x itself."""
+    """act(x) (None with y=False) and the checkpoint of x in 8 bits (anakin_ckpt_forward); `out` may be x itself.  The result has no grad_fn, whatever x has: in a
+    network under autograd the gradient would end here.  Its backward pass is ckpt_backward."""
     res, codes, scales = _host.ckpt_forward(x, _one_of(ACTS, "act", act), y, out)
     return res, Checkpoint(codes, scales, x.shape[1])
 
