@@ -422,7 +422,7 @@ typedef struct anakin_preference_objective {
 /*
  * Log-probability of every row's token, and the entropy of its distribution.
  *   out  logp f32[rows]; entropy f32[rows] or NULL; norm f32[rows][2] or NULL, which the gradient needs: the largest logit m, and log sum exp(scale x - M)
- *        with M an fp32 rounding of scale m (or scale m itself, where that is large).  scale m + the second is the row's log-sum-exp but for a rounding
+ *        with M an fp32 rounding of scale m (or scale m itself, where that is large and in short rows).  scale m + the second is the row's log-sum-exp but for a rounding
  *        of its size.
  * No workspace.  Offsets are not looked at.
  */

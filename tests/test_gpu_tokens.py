@@ -611,7 +611,7 @@ def check_fused(tk, x, tokens, scale, g):
     return got
 
 
-@pytest.mark.parametrize("far", [-1e4, -1e9, -1e10, -1e12, -1e15, -1e20, -1e26, 1e6, 1e10])
+@pytest.mark.parametrize("far", [-1e4, -1e9, -1e10, -1e12, -1e15, -1e20, -1e26, 1e6, 2907270.0, 1e10])  # (2907270 log2(e) is about 2^22)
 @pytest.mark.parametrize("R", [14, 161])
 @pytest.mark.parametrize("V", [4, 100, 200, 1000, 9000, 40000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
